@@ -15,6 +15,7 @@ Modules:
   ucs_ffn -- FFN-pruning saliency and leakage on the retained rows (Eq. 8-9)
   layer_gap -- layer-skipping redundancy gap of input/output cosines (Eq. 7)
   attention -- attention over the packed retained tokens (compressed KV cache)
+  paged -- the compressed cache in pages: reservation, 8-bit values, attention
 
 Readings of points the paper leaves open (scorer MLP form, segment boundaries,
 rounding of K, tie-break, packed order, no score scaling) are stated in the
@@ -25,11 +26,11 @@ function docstrings that use them. Every function here is pinned by the
 from .score import segment_of, silu, sigmoid, score, score_rows
 from .select import num_keep, order_key, select
 from .block import activations, ffn, routed_block, dense_block, routed_rows
-from . import stability, ucs_ffn, layer_gap, attention
+from . import stability, ucs_ffn, layer_gap, attention, paged
 
 __all__ = [
     "segment_of", "silu", "sigmoid", "score", "score_rows",
     "num_keep", "order_key", "select",
     "activations", "ffn", "routed_block", "dense_block", "routed_rows",
-    "stability", "ucs_ffn", "layer_gap", "attention",
+    "stability", "ucs_ffn", "layer_gap", "attention", "paged",
 ]

@@ -21,6 +21,10 @@ built.
                            FFN-pruning saliency / leakage on the retained rows (Eq. 8-9)
     ce_layer_gap           layer-skipping redundancy gap of input/output cosines (Eq. 7)
     ce_routed_attention    attention over the packed retained tokens (compressed KV cache)
+    ce_kv_reserve, ce_kv_append, ce_paged_attention
+                           the compressed cache in pages (bf16 or e4m3): pages and slots for a step's
+                           new rows, made on the device; their keys and values into them; attention
+                           of the new rows over the cache
 """
 from __future__ import annotations
 
@@ -37,6 +41,8 @@ CE_F32, CE_BF16 = 0, 1
 CE_TOK_GEN, CE_TOK_KEEP = 1, 2
 CE_DEV_BAD_OFFSETS, CE_DEV_OVERFLOW = 1, 2
 CE_WS_TOPK, CE_WS_FFN, CE_WS_BLOCK, CE_WS_BLOCK_GAP, CE_WS_FFN_PRUNED, CE_WS_SCORE = 0, 1, 2, 3, 4, 5
+CE_E4M3 = 2
+CE_DEV_NO_PAGES, CE_DEV_TOO_LONG, CE_DEV_BAD_CACHE = 4, 8, 16
 
 EXPORTED = [
     "ce_status_string", "ce_version", "ce_num_keep", "ce_kept_count_host", "ce_workspace_size",
@@ -92,6 +98,17 @@ class CEAttn(ctypes.Structure):
                 ("causal", _i32), ("scale", ctypes.c_float), ("dtype", _i32)]
 
 
+class CEKVCache(ctypes.Structure):
+    _fields_ = [("B", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("page_size", _i32), ("n_pages", _i32),
+                ("max_pages", _i32), ("dtype", _i32), ("page_stride", ctypes.c_int64), ("k", _p), ("v", _p),
+                ("k_scale", _p), ("v_scale", _p), ("page_table", _p)]
+
+
+class CEPagedAttn(ctypes.Structure):
+    _fields_ = [("n_heads", _i32), ("q_capacity", _i32), ("q_offsets", _p), ("lens", _p), ("causal", _i32),
+                ("scale", ctypes.c_float)]
+
+
 def _sig(name, res, args):
     f = getattr(lib, name)
     f.restype = res
@@ -135,6 +152,11 @@ _sig("ce_ffn_mask_channels", ctypes.c_int, [ctypes.POINTER(CEBatch), _p, _p, cty
 _sig("ce_routed_attention", ctypes.c_int, [ctypes.POINTER(CEAttn), _p, _p, _p, _p, _p])
 _sig("ce_attention_workspace_size", ctypes.c_size_t, [ctypes.POINTER(CEAttn)])
 _sig("ce_routed_attention_ws", ctypes.c_int, [ctypes.POINTER(CEAttn), _p, _p, _p, _p, _p, ctypes.c_size_t, _p])
+_sig("ce_kv_reserve", ctypes.c_int, [ctypes.POINTER(CEKVCache), _p, _p, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _p])
+_sig("ce_kv_append", ctypes.c_int, [ctypes.POINTER(CEKVCache), _p, ctypes.c_int64, _p, ctypes.c_int64, _p, _i32, _p])
+_sig("ce_paged_workspace_size", ctypes.c_size_t, [ctypes.POINTER(CEKVCache), ctypes.POINTER(CEPagedAttn)])
+_sig("ce_paged_attention", ctypes.c_int, [ctypes.POINTER(CEKVCache), ctypes.POINTER(CEPagedAttn), _p, ctypes.c_int64,
+                                          _p, _p, ctypes.c_size_t, _p])
 _sig("ce_score_tiling", ctypes.c_int, [ctypes.POINTER(CEBatch), ctypes.POINTER(CEScorerW), _p])
 _sig("ce_layer_gap", ctypes.c_int, [ctypes.POINTER(CEBatch), _p, _p, ctypes.c_int, _i32, _p, ctypes.c_float,
                                     _p, _p, _p, _p, _p, _p])
@@ -704,6 +726,150 @@ def ce_routed_attention(q, k, v, o, q_offsets, kv_offsets, causal, scale, stream
                                       _stream(stream)), "ce_routed_attention")
 
 
+# ----------------------------------------------------------------------------
+# the paged key/value cache (include/ce_router_paged.h)
+# ----------------------------------------------------------------------------
+
+@dataclass
+class KVCache:
+    """A paged cache: k, v [n_pages, H_kv, page_size, 128] bf16, or float8_e4m3fn with
+    float32 scales [H_kv] (or None: 1); page_table int32 [B, max_pages]. The pages
+    of k and v may lie apart (a view of an allocation that holds several layers),
+    everything inside a page is contiguous."""
+    k: "object"
+    v: "object"
+    page_table: "object"
+    k_scale: "object" = None
+    v_scale: "object" = None
+
+    def c(self) -> CEKVCache:
+        k, v, table = self.k, self.v, self.page_table
+        if k is None or v is None or k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("k and v must be [n_pages, kv_heads, page_size, head_dim] of one shape")
+        n, h, page, d = k.shape
+        code = CE_E4M3 if k.dtype is torch.float8_e4m3fn else CE_BF16
+        if table is None or table.dim() != 2:
+            raise ValueError("page_table must be a matrix [B, max_pages]")
+        ptrs = [_chk_strided(x, name, torch.bfloat16 if code == CE_BF16 else torch.float8_e4m3fn, (page * d, d, 1), 16)
+                for name, x in (("k", k), ("v", v))]
+        ld = k.stride(0) if n > 1 else h * page * d
+        if n > 1 and v.stride(0) != ld:
+            raise ValueError("k and v must have pages equally far apart")
+        for name, x in (("k_scale", self.k_scale), ("v_scale", self.v_scale)):
+            if x is not None:
+                ptrs.append(_chk(x, name, _F32, None, (h,)))
+            else:
+                ptrs.append(None)
+        return CEKVCache(table.shape[0], h, d, page, n, table.shape[1], code, ld, ptrs[0], ptrs[1], ptrs[2], ptrs[3],
+                         _chk(table, "page_table", _I32))
+
+
+def _chk_strided(x, name, dtype, strides, unit):
+    """A device tensor whose first dimension may have any stride (a multiple of
+    `unit` elements, no overlap) and the others `strides`; returns its pointer.
+    Strides of dimensions of size 1 say nothing."""
+    if not isinstance(x, torch.Tensor):
+        raise ValueError(f"{name}: expected a torch.Tensor, got {type(x).__name__}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: tensor must live in GPU memory")
+    if x.get_device() != _device():
+        raise ValueError(f"{name}: tensor is on {x.device}, the current device is cuda:{_device()}")
+    if x.dtype is not dtype:
+        raise ValueError(f"{name}: dtype {x.dtype}, expected {dtype}")
+    shape, st = x.shape, x.stride()
+    if any(n > 1 and a != b for n, a, b in zip(shape[1:], st[1:], strides)):
+        raise ValueError(f"{name}: strides {st}: only the first dimension may be spaced")
+    if shape[0] > 1 and (st[0] < shape[1] * strides[0] or st[0] % unit):
+        raise ValueError(f"{name}: first stride {st[0]} must be a multiple of {unit} and at least {shape[1] * strides[0]}")
+    p = x.data_ptr()
+    if p & 15 and x.numel():
+        raise ValueError(f"{name}: data pointer is not 16-byte aligned")
+    return p
+
+
+def _rows3(x, name, heads=None):
+    """Rows [n, heads, 128] bf16 of a packed batch, possibly a part of wider rows: pointer, rows, stride in elements."""
+    if x is None or x.dim() != 3 or (heads is not None and x.shape[1] != heads):
+        raise ValueError(f"{name} must be [rows, {'heads' if heads is None else heads}, head_dim]")
+    n, h, d = x.shape
+    return _chk_strided(x, name, torch.bfloat16, (d, 1), 8), n, x.stride(0) if n > 1 else h * d
+
+
+def ce_kv_reserve(cache: KVCache, lens, new_offsets, free_pages, free_count, start, slots, lens_out=None,
+                  free_count_out=None, reset=None, status=None, stream=None):
+    """Pages and slots for every sequence's new rows; sequences marked in `reset` give
+    theirs back first. lens_out and free_count_out default to lens and free_count (in
+    place). new_offsets None: no new rows (slots may be None). slots holds as many
+    entries as rows can come; status: 4-byte integer tensor for the CE_DEV_* bits."""
+    cc = cache.c()
+    B = cc.B
+    rows = 0 if slots is None else slots.numel()
+    if new_offsets is None and rows:
+        raise ValueError("slots without new_offsets")
+    if status is not None and status.dtype not in (torch.int32, torch.uint32):
+        raise ValueError("status must be a 4-byte integer tensor")
+    lp, cp = _chk(lens, "lens", _I32, None, (B,)), _chk(free_count, "free_count", _I32, None, (1,))
+    _check(lib.ce_kv_reserve(
+        ctypes.byref(cc), lp, None if new_offsets is None else _chk(new_offsets, "new_offsets", _I32, None, (B + 1,)),
+        rows, None if reset is None else _chk(reset, "reset", _U8, None, (B,)),
+        _chk(free_pages, "free_pages", _I32, None, (cc.n_pages,)), cp,
+        lp if lens_out is None else _chk(lens_out, "lens_out", _I32, None, (B,)),
+        cp if free_count_out is None else _chk(free_count_out, "free_count_out", _I32, None, (1,)),
+        _chk(start, "start", _I32, None, (B,)), None if not rows else _chk(slots, "slots", _I32, None, (rows,)),
+        _chk(status, "status", numel=1, optional=True), _stream(stream)), "ce_kv_reserve")
+
+
+def ce_kv_append(cache: KVCache, k_new, v_new, slots, stream=None):
+    """k_new, v_new [rows, H_kv, 128] bf16 (rows may be spaced, as in a fused projection)
+    into their slots (ce_kv_reserve; -1 is skipped)."""
+    cc = cache.c()
+    kp, n, kld = _rows3(k_new, "k_new", cc.n_kv_heads)
+    vp, nv, vld = _rows3(v_new, "v_new", cc.n_kv_heads)
+    if nv != n or k_new.shape[2] != cc.head_dim or v_new.shape[2] != cc.head_dim:
+        raise ValueError("k_new and v_new must have the same rows and the cache's head_dim")
+    _check(lib.ce_kv_append(ctypes.byref(cc), kp, kld, vp, vld, _chk(slots, "slots", _I32, None, (n,)), n,
+                            _stream(stream)), "ce_kv_append")
+
+
+def _paged_attn(cc, q_rows, heads, q_offsets=None, lens=None, causal=0, scale=1.0):
+    return CEPagedAttn(heads, q_rows, q_offsets, lens, int(bool(causal)), float(scale))
+
+
+def ce_paged_workspace_size(cache: KVCache, q_rows: int, n_heads: int) -> int:
+    cc = cache.c()
+    return int(lib.ce_paged_workspace_size(ctypes.byref(cc), ctypes.byref(_paged_attn(cc, int(q_rows), int(n_heads)))))
+
+
+def alloc_paged_workspace(cache: KVCache, q_rows: int, n_heads: int):
+    """Workspace of ce_paged_attention for up to q_rows rows of n_heads heads, on the cache's device."""
+    return torch.empty(max(ce_paged_workspace_size(cache, q_rows, n_heads), 256), dtype=torch.uint8,
+                       device=cache.k.device)
+
+
+def ce_paged_attention(cache: KVCache, q, o, q_offsets, lens, causal, scale, ws=None, stream=None):
+    """q [rows, H, 128] bf16 (rows may be spaced) over the cache's first lens[b] tokens of
+    each sequence, o [rows, H, 128]; q_offsets int32 [B+1], lens int32 [B]. Without
+    a workspace (alloc_paged_workspace) scratch comes from torch's allocator."""
+    cc = cache.c()
+    qp, n, ld = _rows3(q, "q")
+    if q.shape[2] != cc.head_dim:
+        raise ValueError(f"q: head_dim {q.shape[2]}, the cache has {cc.head_dim}")
+    at = _paged_attn(cc, n, q.shape[1], _chk(q_offsets, "q_offsets", _I32, None, (cc.B + 1,)),
+                     _chk(lens, "lens", _I32, None, (cc.B,)), causal, scale)
+    need = int(lib.ce_paged_workspace_size(ctypes.byref(cc), ctypes.byref(at)))
+    if ws is None and need:
+        # stream-ordered scratch, on the stream that the kernels run on (any object
+        # with a raw handle is a stream here, as in every call)
+        with torch.cuda.stream(torch.cuda.current_stream() if stream is None else
+                               stream if isinstance(stream, torch.cuda.Stream) else
+                               torch.cuda.ExternalStream(stream.cuda_stream)):
+            ws = torch.empty(need, dtype=_U8, device=q.device)
+    wp, wn = (None, 0) if ws is None else _ws_ptr(ws, need)
+    _check(lib.ce_paged_attention(ctypes.byref(cc), ctypes.byref(at), qp, ld,
+                                  _chk(o, "o", torch.bfloat16, None, q.shape), wp, wn, _stream(stream)),
+           "ce_paged_attention")
+
+
 __all__ = [
     "Batch", "Scorer", "FFN", "CERouterError", "lib", "alloc_workspace",
     "ce_version", "ce_num_keep", "ce_kept_count_host", "ce_workspace_size", "ce_workspace_status",
@@ -712,6 +878,8 @@ __all__ = [
     "ce_scatter_residual", "ce_routed_block", "ce_routed_block_gap", "ce_drop_stability",
     "ce_ffn_down_colnorms", "ce_ffn_saliency", "ce_ffn_mask_channels", "ce_layer_gap",
     "ce_routed_attention", "CEAttn",
+    "KVCache", "ce_kv_reserve", "ce_kv_append", "ce_paged_attention", "ce_paged_workspace_size",
+    "alloc_paged_workspace", "CE_E4M3", "CE_DEV_NO_PAGES", "CE_DEV_TOO_LONG", "CE_DEV_BAD_CACHE",
     "CE_F32", "CE_BF16", "CE_TOK_GEN", "CE_TOK_KEEP", "CE_WS_TOPK", "CE_WS_FFN", "CE_WS_BLOCK", "CE_WS_BLOCK_GAP",
     "CE_WS_FFN_PRUNED", "CE_WS_SCORE",
     "CE_DEV_BAD_OFFSETS", "CE_DEV_OVERFLOW",

@@ -1,0 +1,69 @@
+// The paged key/value cache between its C entry points and its kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ce_router_paged.h"
+
+namespace ce {
+
+struct ReserveArgs {
+  int B, max_pages, n_pages, page_log2, rows;
+  const int32_t* lens;
+  const int32_t* offs;   // or NULL
+  const uint8_t* reset;  // or NULL
+  int32_t* table;
+  int32_t* free_pages;
+  const int32_t* count;
+  int32_t* lens_out;
+  int32_t* count_out;
+  int32_t* start;
+  int32_t* slots;
+  uint32_t* status;  // or NULL
+  int slots_apart;   // the slots come from a launch of their own
+};
+
+struct AppendArgs {
+  const char *k_new, *v_new;
+  int64_t k_ld, v_ld;  // bytes between rows
+  const int32_t* slots;
+  int rows, Hkv, n_slots, page_log2;
+  char *k, *v;
+  int64_t page_bytes;  // between pages
+  const float *k_scale, *v_scale;
+};
+
+struct PagedArgs {
+  const char* q;
+  char* o;
+  const char *k, *v;
+  const float *ks, *vs;  // scales of 8-bit pages, or NULL
+  const int32_t *table, *qo, *lens;
+  int64_t q_ld;        // bytes between rows of q
+  int64_t page_bytes;  // bytes between pages
+  int B, H, Hkv, q_cap, n_pages, max_pages, page_log2, causal;
+  float scale_log2;  // scale * log2(e)
+  float* part;       // partial results, kPagedPart floats a slot
+  int64_t* plan;     // B > kPagedScan: prefix sums of the sequences' items, then the chunk length
+};
+
+constexpr int kPagedScan = 256;    // sequences that a wave plans by itself (four a lane)
+constexpr int kPagedTarget = 512;  // workgroups that the cut sequences are cut into: two on each CU
+constexpr int kPagedRows = 128;    // (query, head) rows of a tile
+constexpr int kPagedPart = kPagedRows * (128 + 2);  // floats of a slot: outputs, maxima, sums
+
+// What the host knows of a call: the workgroups that any batch of these sizes needs.
+struct PagedGrid {
+  int64_t items;   // workgroups over all key/value heads
+  int tiles;       // cut row tiles of a key/value head, at most (0: no sequence is cut)
+  int rows;        // rows of one, at most
+  size_t plan_bytes, bytes;
+};
+PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys);
+
+hipError_t launch_kv_reserve(ReserveArgs a, hipStream_t stream);
+hipError_t launch_kv_append(const AppendArgs& a, bool e4m3, hipStream_t stream);
+hipError_t launch_paged_attention(const PagedArgs& a, bool e4m3, hipStream_t stream);
+
+}  // namespace ce
