@@ -34,6 +34,11 @@ struct AppendArgs {
   const float *k_scale, *v_scale;
 };
 
+// Items and partial results of the sequences before one, and its units that are not cut.
+struct PagedPlan {
+  uint32_t items, slots, whole;
+};
+
 struct PagedArgs {
   const char* q;
   char* o;
@@ -44,26 +49,29 @@ struct PagedArgs {
   int64_t page_bytes;  // bytes between pages
   int B, H, Hkv, q_cap, n_pages, max_pages, page_log2, causal;
   float scale_log2;  // scale * log2(e)
+  uint32_t grid;     // items that the launch has workgroups for
   float* part;       // partial results, kPagedPart floats a slot
-  int64_t* plan;     // B > kPagedScan: prefix sums of the sequences' items, then the chunk length
+  unsigned long long* arrived;  // counters of the chunks that meet, kPagedTarget a level
+  unsigned long long token;     // of this call, 48 bits
+  PagedPlan* plan;   // B > kPagedScan: the sequences, then the totals and (whole) the chunk length
 };
 
 constexpr int kPagedScan = 256;    // sequences that a wave plans by itself (four a lane)
-constexpr int kPagedTarget = 512;  // workgroups that the cut sequences are cut into: two on each CU
+constexpr int kPagedTarget = 512;  // places for workgroups: two on each CU
 constexpr int kPagedRows = 128;    // (query, head) rows of a tile
 constexpr int kPagedPart = kPagedRows * (128 + 2);  // floats of a slot: outputs, maxima, sums
 
+constexpr int kPagedLevels = 3;     // eight or sixteen chunks meet at a time, 512 at most
+
 // What the host knows of a call: the workgroups that any batch of these sizes needs.
 struct PagedGrid {
-  int64_t items;   // workgroups over all key/value heads
-  int tiles;       // cut row tiles of a key/value head, at most (0: no sequence is cut)
-  int rows;        // rows of one, at most
-  size_t plan_bytes, bytes;
+  int64_t items;
+  size_t plan_bytes, count_bytes, bytes;  // workspace: the plan, arrival counters, partial results
 };
 PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys);
 
 hipError_t launch_kv_reserve(ReserveArgs a, hipStream_t stream);
 hipError_t launch_kv_append(const AppendArgs& a, bool e4m3, hipStream_t stream);
-hipError_t launch_paged_attention(const PagedArgs& a, bool e4m3, hipStream_t stream);
+hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream);
 
 }  // namespace ce

@@ -157,8 +157,10 @@ int ce_paged_attention(const ce_kv_cache* cache, const ce_paged_attn* attn, cons
   a.page_log2 = log2_of_page(cache->page_size);
   a.causal = attn->causal;
   a.scale_log2 = attn->scale * 1.4426950408889634f;
-  a.plan = static_cast<int64_t*>(ws);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + p.plan_bytes);
+  char* const w = static_cast<char*>(ws);
+  a.plan = reinterpret_cast<PagedPlan*>(w);
+  a.arrived = reinterpret_cast<unsigned long long*>(w + p.plan_bytes);
+  a.part = reinterpret_cast<float*>(w + p.plan_bytes + p.count_bytes);
   return hip_status(launch_paged_attention(a, cache->dtype == CE_E4M3, static_cast<hipStream_t>(stream)));
 }
 

@@ -20,6 +20,8 @@ constexpr int kKBytes = kKT * kRowB;
 constexpr int kAhead = 3;          // MFMA operands read from LDS this many products ahead
 constexpr float kLazy = 8.0f;      // headroom of the running maximum (exponent of 2)
 constexpr int kMinChunk = 256;     // least keys of a chunk
+constexpr int kMeet = 16;          // chunks that meet at a time: paged_few
+constexpr int kMeetTile = 8;       // and paged_tile
 constexpr int kOLd = kDh + 4;      // floats per row of paged_few's outputs in LDS
 constexpr int kVRow = kBK * 2;     // bytes per row of paged_few's V^T
 constexpr int kVTile = kDh * kVRow;
@@ -29,20 +31,32 @@ static_assert(kSmem >= 4 * kKBytes && kSmem >= 4 * kVTile, "the tiles fit");
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
 // ------------------------------------------------------------------ the plan
+//
+// A unit is a row tile of a sequence for one key/value head; units are numbered
+// sequence by sequence, head by head, the last tiles first (under a causal mask they
+// see the most keys). With S = 512 places for workgroups (two on each CU) and
+// A = (sum of the units' keys) / S:
+//   * a batch of many units fills S places some whole number of times and leaves
+//     a rest; the units before the rest are whole, and the rest, fewer than S, are cut
+//     along their keys so that they too fill the places: L = (their keys) / S;
+//   * where one sequence alone has 2 A keys or more, or there are fewer units than
+//     places, every unit may be cut, L = A.
+// A unit of n_k keys is cut into floor(n_k / L) chunks, so the chunks of all cut units
+// are at most S (a second round of a few would double the time) and as many
+// partial results fit the workspace.
 
 struct Size {
   int qbase, nq, nk, tiles;
-  bool few;
 };
+
+__device__ __forceinline__ bool is_few(int nq, int g) { return nq * g <= kFew; }
 
 __device__ __forceinline__ Size size_from(const PagedArgs& a, int q0, int q1, int len, int g) {
   Size s;
   s.qbase = clampi(q0, 0, a.q_cap);
   s.nq = clampi(q1, s.qbase, a.q_cap) - s.qbase;
   s.nk = clampi(len, 0, a.max_pages << a.page_log2);
-  const int rows = s.nq * g;
-  s.few = rows <= kFew;
-  s.tiles = s.few ? (rows > 0 ? 1 : 0) : (rows + kPagedRows - 1) / kPagedRows;
+  s.tiles = (s.nq * g + kPagedRows - 1) / kPagedRows;
   return s;
 }
 
@@ -50,47 +64,56 @@ __device__ __forceinline__ Size size_of(const PagedArgs& a, int b, int g) {
   return size_from(a, a.qo[b], a.qo[b + 1], a.lens[b], g);
 }
 
-// Keys per chunk for a batch of w tile-keys.
-__device__ __forceinline__ int chunk_length(const PagedArgs& a, int64_t w) {
-  const int64_t l = (w * a.Hkv + kPagedTarget - 1) / kPagedTarget;
-  return (int)(l < kMinChunk ? kMinChunk : l > (1 << 30) ? 1 << 30 : l);
+// Units before the rest, of n in all with w keys, the longest of which has `longest`.
+__device__ __forceinline__ uint32_t whole_units(uint32_t n, float w, int longest) {
+  return (float)longest * (0.5f * kPagedTarget) >= w ? 0 : n / kPagedTarget * kPagedTarget;
+}
+
+// Keys per chunk where the units that may be cut have w keys.
+__device__ __forceinline__ int chunk_length(float w) {
+  const float l = w * (1.0f / kPagedTarget);
+  return l < (float)kMinChunk ? kMinChunk : l > 1e9f ? 1 << 30 : (int)l + 1;
 }
 
 // A sequence's chunks (a whole number of the tiles that its waves take in turn).
-__device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int L, int& C, int& chunk) {
-  C = kPagedTarget / a.Hkv >= 2 ? s.nk / L : 1;
-  if (C <= 1) {
-    C = 1;
-    chunk = s.nk;
-    return;
+__device__ __forceinline__ void cut(const Size& s, int g, int L, int& C, int& chunk) {
+  C = s.nk / L;
+  chunk = s.nk;
+  if (C > 1) {
+    const int unit = is_few(s.nq, g) ? 4 * kBK : kKT;
+    chunk = (int)(((uint32_t)s.nk + C - 1) / (uint32_t)C + unit - 1) / unit * unit;
+    C = (int)(((uint32_t)s.nk + chunk - 1) / (uint32_t)chunk);
   }
-  const int unit = s.few ? 4 * kBK : kKT;
-  chunk = (int)(((uint32_t)s.nk + C - 1) / (uint32_t)C + unit - 1) / unit * unit;
-  C = (int)(((uint32_t)s.nk + chunk - 1) / (uint32_t)chunk);
   if (C <= 1) {
     C = 1;
     chunk = s.nk;
   }
 }
 
-// Items of a sequence and key/value head, and where it is cut its partial
-// results (from bit 32) and row tiles (from bit 48).
-__device__ __forceinline__ int64_t counts_of(const PagedArgs& a, const Size& s, int L) {
+// Of a sequence whose units begin at number `first`: those that stay whole.
+__device__ __forceinline__ uint32_t whole_of(const PagedArgs& a, const Size& s, uint32_t first, uint32_t whole) {
+  const uint32_t n = (uint32_t)s.tiles * a.Hkv;
+  return whole <= first ? 0 : min(n, whole - first);
+}
+
+// Its items, and its partial results.
+__device__ __forceinline__ void counts_of(const PagedArgs& a, const Size& s, int g, int L, uint32_t whole, uint32_t& items,
+                                          uint32_t& slots) {
   int C, chunk;
-  cut(a, s, L, C, chunk);
-  const int64_t n = (int64_t)s.tiles * C;
-  return n | (C > 1 ? (n & 0xffff) << 32 | (int64_t)(s.tiles & 0x7fff) << 48 : 0);
+  cut(s, g, L, C, chunk);
+  const uint32_t n = (uint32_t)s.tiles * a.Hkv;
+  slots = C > 1 ? (n - whole) * C : 0;
+  items = C > 1 ? whole + slots : n;
 }
 
 struct Item {
   int b, kvh, qbase, nq, nk;
   bool few;
-  int tile, C, chunk;   // row tile, chunks of the sequence, keys of each
-  int c;                // chunk of this item
-  int slot;             // first partial result of the sequence (per key/value head)
-  int rows;             // rows of the tile
-  int vis_end;          // keys that its last row sees
-  int tile_chunks;      // chunks that hold keys it sees (1: no partial results)
+  int tile, chunk;   // row tile, keys per chunk
+  int c, n_chunks;   // chunk of this item, of those that hold keys its rows see (1: no partial results)
+  int slot;          // partial result of its first chunk
+  int rows;          // rows of the tile
+  int vis_end;       // keys that its last row sees
 };
 
 // Keys [0, row_limit) of the first `end` are seen by query qi.
@@ -99,154 +122,193 @@ __device__ __forceinline__ int row_limit(const PagedArgs& a, const Item& it, int
   return clampi(it.nk - it.nq + qi + 1, 0, end);
 }
 
-
-__device__ __forceinline__ int64_t readlane64(int64_t x, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane);
-  const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)((uint64_t)x >> 32), lane);
-  return (int64_t)((uint64_t)hi << 32 | lo);
+// Inclusive prefix sum over the wave (row shifts, then the rows' last lanes).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
 }
 
-// Index `at` among the prefix sums' items or cut tiles.
-template <bool kCutTiles>
-__device__ __forceinline__ int key_of(int64_t prefix) {
-  return kCutTiles ? (int)(prefix >> 48) : (int)(uint32_t)prefix;
+// Sum over the wave, in the same order in every wave (0 is what a lane without a
+// neighbour adds).
+__device__ __forceinline__ float wave_sum(float v) {
+#define CE_STEP(ctrl, rows) \
+  v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, rows, 0xf, false))
+  CE_STEP(0x111, 0xf);
+  CE_STEP(0x112, 0xf);
+  CE_STEP(0x114, 0xf);
+  CE_STEP(0x118, 0xf);
+  CE_STEP(0x142, 0xa);
+  CE_STEP(0x143, 0xc);
+#undef CE_STEP
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
-// The sequence that holds item (or cut tile) number `at` of a key/value head, its
-// sizes, the prefix sums before it and the chunk length; false past the last.
-// Every wave finds it by itself, kPer sequences a lane.
-template <bool kCutTiles, int kPer>
-__device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, int at, int& b, Size& size, int64_t& before,
-                                             int& L) {
+// Largest of non-negative values over the wave.
+__device__ __forceinline__ int wave_max(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// The sequence that holds an item, and what was counted before it.
+struct Found {
+  int b, L;
+  Size size;
+  uint32_t whole;         // its units that stay whole
+  uint32_t items, slots;  // of the sequences before
+};
+
+// The sequence of item `at`; false past the last. Every wave finds it by itself, kPer
+// sequences a lane.
+template <int kPer>
+__device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t at, Found& f) {
   const int lane = threadIdx.x & 63;
   Size s[kPer];
-  int64_t w = 0;
+  float w = 0.0f;
+  uint32_t units = 0;
+  int longest = 0;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int bb = lane * kPer + i;
-    s[i] = Size{0, 0, 0, 0, true};
-    if (bb < a.B) s[i] = size_of(a, bb, g);
-    w += (int64_t)s[i].tiles * s[i].nk;
+    const int b = lane * kPer + i;
+    s[i] = Size{0, 0, 0, 0};
+    if (b < a.B) s[i] = size_of(a, b, g);
+    const uint32_t n = (uint32_t)s[i].tiles * a.Hkv;
+    w += (float)n * (float)s[i].nk;
+    units += n;
+    longest = max(longest, n ? s[i].nk : 0);
   }
+  const uint32_t units_to = wave_scan(units);
+  w = wave_sum(w);
+  const uint32_t all = __builtin_amdgcn_readlane(units_to, 63);
+  uint32_t whole = whole_units(all, w, wave_max(longest));
+  if (whole) {  // the rest's keys
+    float rest = 0.0f;
+    uint32_t first = units_to - units;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) w += __shfl_xor(w, o);
-  L = chunk_length(a, w);
-  int64_t v[kPer], sum = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    v[i] = counts_of(a, s[i], L);
-    sum += v[i];
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t n = (uint32_t)s[i].tiles * a.Hkv;
+      rest += (float)(n - whole_of(a, s[i], first, whole)) * (float)s[i].nk;
+      first += n;
+    }
+    w = wave_sum(rest);
   }
-  int64_t x = sum;
+  f.L = chunk_length(w);
+  uint32_t items[kPer], slots[kPer], wh[kPer], sum_i, sum_s, items_to, slots_to;
+  for (;;) {
+    sum_i = sum_s = 0;
+    uint32_t first = units_to - units;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o);
-    if (lane >= o) x += y;
+    for (int i = 0; i < kPer; ++i) {
+      wh[i] = whole_of(a, s[i], first, whole);
+      counts_of(a, s[i], g, f.L, wh[i], items[i], slots[i]);
+      first += (uint32_t)s[i].tiles * a.Hkv;
+      sum_i += items[i];
+      sum_s += slots[i];
+    }
+    items_to = wave_scan(sum_i);
+    slots_to = wave_scan(sum_s);
+    // more workgroups than the launch has, or slots than the workspace: only where
+    // offsets are out of order. Then nothing is cut (every chunk of a cut unit
+    // must run) and what lies past the grid is left.
+    if (f.L == 1 << 30 || (__builtin_amdgcn_readlane(items_to, 63) <= a.grid &&
+                           __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedTarget))
+      break;
+    f.L = 1 << 30;
   }
-  const uint64_t past = __builtin_amdgcn_ballot_w64(at < key_of<kCutTiles>(x));
+  const uint64_t past = __builtin_amdgcn_ballot_w64(at < items_to);
   if (!past) return false;
   const int ln = __builtin_ctzll(past);
-  before = readlane64(x - sum, ln);
-  L = __builtin_amdgcn_readfirstlane(L);
+  f.items = __builtin_amdgcn_readlane(items_to - sum_i, ln);
+  f.slots = __builtin_amdgcn_readlane(slots_to - sum_s, ln);
   bool found = false;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int64_t vi = readlane64(v[i], ln);
-    if (!found) {
-      if (i == kPer - 1 || at < key_of<kCutTiles>(before + vi)) {
-        found = true;
-        b = ln * kPer + i;
-        size.qbase = __builtin_amdgcn_readlane(s[i].qbase, ln);
-        size.nq = __builtin_amdgcn_readlane(s[i].nq, ln);
-        size.nk = __builtin_amdgcn_readlane(s[i].nk, ln);
-        size.tiles = __builtin_amdgcn_readlane(s[i].tiles, ln);
-        size.few = size.nq * g <= kFew;
-      } else {
-        before += vi;
-      }
+    const uint32_t ni = __builtin_amdgcn_readlane(items[i], ln);
+    if (found) continue;
+    if (i == kPer - 1 || at < f.items + ni) {
+      found = true;
+      f.b = ln * kPer + i;
+      f.size.qbase = __builtin_amdgcn_readlane(s[i].qbase, ln);
+      f.size.nq = __builtin_amdgcn_readlane(s[i].nq, ln);
+      f.size.nk = __builtin_amdgcn_readlane(s[i].nk, ln);
+      f.size.tiles = __builtin_amdgcn_readlane(s[i].tiles, ln);
+      f.whole = __builtin_amdgcn_readlane(wh[i], ln);
+    } else {
+      f.items += ni;
+      f.slots += __builtin_amdgcn_readlane(slots[i], ln);
     }
   }
   return true;
 }
 
 // The same from the plan in memory: three rounds of 64 samples.
-template <bool kCutTiles>
-__device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, int at, int& b, Size& size, int64_t& before,
-                                             int& L) {
+__device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, uint32_t at, Found& f) {
   const int lane = threadIdx.x & 63;
-  if (at >= key_of<kCutTiles>(a.plan[a.B])) return false;
-  int lo = 0;  // the last sequence whose prefix is at most `at` is in [lo, lo + 64 step)
+  if (at >= a.plan[a.B].items) return false;
+  int lo = 0;  // the last sequence whose items begin at or before `at` is in [lo, lo + 64 step)
 #pragma unroll
   for (int step = 4096; step > 0; step >>= 6) {
     const int i = lo + lane * step;
-    const bool le = i < a.B && key_of<kCutTiles>(a.plan[i < a.B ? i : 0]) <= at;
+    const bool le = i < a.B && a.plan[i < a.B ? i : 0].items <= at;
     const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(le));
     lo += (n > 0 ? n - 1 : 0) * step;
   }
-  b = __builtin_amdgcn_readfirstlane(lo);
-  before = readlane64(a.plan[b], 0);
-  L = __builtin_amdgcn_readfirstlane((int)a.plan[a.B + 1]);
-  size = size_of(a, b, g);
-  size.qbase = __builtin_amdgcn_readfirstlane(size.qbase);
-  size.nq = __builtin_amdgcn_readfirstlane(size.nq);
-  size.nk = __builtin_amdgcn_readfirstlane(size.nk);
-  size.tiles = __builtin_amdgcn_readfirstlane(size.tiles);
-  size.few = size.nq * g <= kFew;
+  f.b = __builtin_amdgcn_readfirstlane(lo);
+  const PagedPlan p = a.plan[f.b];
+  f.items = __builtin_amdgcn_readfirstlane(p.items);
+  f.slots = __builtin_amdgcn_readfirstlane(p.slots);
+  f.whole = __builtin_amdgcn_readfirstlane(p.whole);
+  f.L = __builtin_amdgcn_readfirstlane((int)a.plan[a.B].whole);
+  const Size s = size_of(a, f.b, g);
+  f.size.qbase = __builtin_amdgcn_readfirstlane(s.qbase);
+  f.size.nq = __builtin_amdgcn_readfirstlane(s.nq);
+  f.size.nk = __builtin_amdgcn_readfirstlane(s.nk);
+  f.size.tiles = __builtin_amdgcn_readfirstlane(s.tiles);
   return true;
 }
 
-template <bool kCutTiles>
-__device__ __forceinline__ bool find(const PagedArgs& a, int g, int at, int& b, Size& size, int64_t& before, int& L) {
-  if (a.B <= 64) return find_by_scan<kCutTiles, 1>(a, g, at, b, size, before, L);
-  if (a.B <= kPagedScan) return find_by_scan<kCutTiles, kPagedScan / 64>(a, g, at, b, size, before, L);
-  return find_in_plan<kCutTiles>(a, g, at, b, size, before, L);
-}
-
-// What a row tile of the sequence sees, and where its partial results go. False
-// if they would lie outside the workspace (only where offsets out of order make
-// the plan's sums meaningless).
-__device__ __forceinline__ bool finish_item(const PagedArgs& a, int g, const Size& s, int64_t before, Item& it) {
-  it.qbase = s.qbase;
-  it.nq = s.nq;
-  it.nk = s.nk;
-  it.few = s.few;
+__device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item& it) {
+  const int g = a.H / a.Hkv;
+  Found f;
+  if (!(a.B <= 64 ? find_by_scan<1>(a, g, at, f)
+                  : a.B <= kPagedScan ? find_by_scan<kPagedScan / 64>(a, g, at, f) : find_in_plan(a, g, at, f)))
+    return false;
+  it.b = f.b;
+  it.qbase = f.size.qbase;
+  it.nq = f.size.nq;
+  it.nk = f.size.nk;
+  it.few = is_few(it.nq, g);
+  int C;
+  cut(f.size, g, f.L, C, it.chunk);
+  uint32_t u = at - f.items;
+  it.c = 0;
+  it.slot = 0;
+  if (C > 1 && u >= f.whole) {
+    const uint32_t v = u - f.whole;
+    const uint32_t back = v / (uint32_t)C;
+    it.c = (int)(v - back * C);
+    it.slot = (int)(f.slots + back * C);
+    u = f.whole + back;
+  } else {
+    C = 1;
+    it.chunk = it.nk;
+  }
+  it.kvh = (int)(u / (uint32_t)f.size.tiles);
+  it.tile = f.size.tiles - 1 - (int)(u - (uint32_t)it.kvh * f.size.tiles);
   const int r0 = it.tile * kPagedRows;
-  it.rows = min(kPagedRows, s.nq * g - r0);
-  it.vis_end = row_limit(a, it, (r0 + it.rows - 1) / g, s.nk);
-  it.tile_chunks = it.C > 1 ? max(1, (it.vis_end + it.chunk - 1) / it.chunk) : 1;
-  it.slot = (int)((before >> 32) & 0xffff);
-  return it.C <= 1 || it.slot + s.tiles * it.C <= kPagedTarget / a.Hkv;
-}
-
-__device__ __forceinline__ bool find_item(const PagedArgs& a, int64_t j, Item& it) {
-  const int g = a.H / a.Hkv;
-  Size s;
-  int64_t before;
-  int L;
-  const int64_t at = j / a.Hkv;
-  if (!find<false>(a, g, (int)at, it.b, s, before, L)) return false;
-  cut(a, s, L, it.C, it.chunk);
-  const int n = s.tiles * it.C;
-  const int rem = (int)(j - (int64_t)key_of<false>(before) * a.Hkv);
-  it.kvh = rem / n;
-  const int sub = rem - it.kvh * n;
-  // last tiles first: under a causal mask they see the most keys
-  const int back = sub / it.C;
-  it.tile = s.tiles - 1 - back;
-  it.c = sub - back * it.C;
-  return finish_item(a, g, s, before, it) && it.c < it.tile_chunks;
-}
-
-__device__ __forceinline__ bool find_cut_tile(const PagedArgs& a, int at, Item& it) {
-  const int g = a.H / a.Hkv;
-  Size s;
-  int64_t before;
-  int L;
-  if (!find<true>(a, g, at, it.b, s, before, L)) return false;
-  cut(a, s, L, it.C, it.chunk);
-  it.tile = at - key_of<true>(before);
-  it.kvh = it.c = 0;
-  return finish_item(a, g, s, before, it);
+  it.rows = min(kPagedRows, it.nq * g - r0);
+  it.vis_end = row_limit(a, it, (r0 + it.rows - 1) / g, it.nk);
+  it.n_chunks = C > 1 ? max(1, (int)(((uint32_t)it.vis_end + it.chunk - 1) / (uint32_t)it.chunk)) : 1;
+  return it.c < it.n_chunks;
 }
 
 // ------------------------------------------------------- softmax and results
@@ -264,15 +326,55 @@ __device__ __forceinline__ float normalizer(float l, float vs, bool sees) {
   return sees ? vs / l : 0.0f;
 }
 
-// Place of dims 4 qd .. +3 of row r in a partial result: rows of 128 floats, or
-// for 128-row tiles the accumulators as the lanes hold them.
-__device__ __forceinline__ int part_offset(bool few, int r, int qd) {
-  if (few) return r * kDh + 4 * qd;
-  return (((r >> 5) * 16 + (qd >> 1)) * 64 + (r & 31) + 32 * (qd & 1)) * 4;
+// Partial results of the chunks of a unit meet through the workspace. Each chunk's
+// workgroup writes its own and arrives; the last of a group of neighbours adds the
+// group up in chunk order, so no result depends on who came last, and goes on as one
+// chunk of the next level. Nobody waits for anybody. The sums move by device-coherent
+// (sc1) stores and loads, and a workgroup arrives when its stores have completed, so
+// no cache is written back or dropped.
+constexpr int kSC1 = 16;            // cache-policy operand: sc1
+constexpr uint32_t kSlotBytes = kPagedPart * 4;
+constexpr uint32_t kStats = kPagedRows * kDh * 4;  // maxima, then sums, behind a slot's outputs
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t part_rsrc(const PagedArgs& a) {
+  return make_rsrc(a.part, (uint32_t)kPagedTarget * kSlotBytes);
+}
+__device__ __forceinline__ void part_store4(__amdgpu_buffer_rsrc_t rs, uint32_t at, float x, float y, float z, float w) {
+  const u32x4_t v = {__float_as_uint(x), __float_as_uint(y), __float_as_uint(z), __float_as_uint(w)};
+  __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)at, 0, kSC1);
+}
+__device__ __forceinline__ void part_store(__amdgpu_buffer_rsrc_t rs, uint32_t at, float x) {
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), rs, (int)at, 0, kSC1);
+}
+__device__ __forceinline__ f32x4_t part_load4(__amdgpu_buffer_rsrc_t rs, uint32_t at) {
+  return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at, 0, kSC1));
+}
+__device__ __forceinline__ float part_load(__amdgpu_buffer_rsrc_t rs, uint32_t at) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (int)at, 0, kSC1));
 }
 
-__device__ __forceinline__ float* part_of(const PagedArgs& a, const Item& it) {
-  return a.part + ((int64_t)(it.slot + it.tile * it.C + it.c) * a.Hkv + it.kvh) * kPagedPart;
+// This workgroup's stores are complete and it arrives at counter `i`: is it the last of
+// n? A counter holds the call's token above the arrivals; any other content, whatever
+// the workspace held before, counts as none, and the last leaves zero (a captured call
+// replays with the same token). `said`: a word of LDS that nobody else uses meanwhile.
+__device__ __forceinline__ bool arrive_last(const PagedArgs& a, int i, int n, int* said) {
+  asm volatile("" ::: "memory");
+  wait_vmcnt<0>();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    unsigned long long* const p = a.arrived + i;
+    unsigned long long old = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), next;
+    do {
+      next = (old >> 16) == a.token ? old + 1 : (a.token << 16) + 1;
+      if ((int)(next & 0xffff) == n) next = 0;
+    } while (!__hip_atomic_compare_exchange_strong(p, &old, next, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT));
+    *said = next == 0;
+  }
+  __syncthreads();
+  const bool last = __builtin_amdgcn_readfirstlane(*said) != 0;
+  __syncthreads();  // read by every wave before it is used again
+  return last;
 }
 
 // 8-byte LDS read that transposes 4 x 16 blocks of 16-bit values inside groups
@@ -603,11 +705,25 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
             f32x4_t{oacc[db][4 * g4] * al, oacc[db][4 * g4 + 1] * al, oacc[db][4 * g4 + 2] * al, oacc[db][4 * g4 + 3] * al};
   }
   __syncthreads();
-  const bool partial = it.tile_chunks > 1;
   const float vs = kF8 && a.vs ? a.vs[kvh] : 1.0f;
-  // thread: row tid / 32 (+ 8, 16, 24), dims 4 (tid % 32) .. +3
-  for (int r = tid_e >> 5; r < rows; r += 8) {
-    const int qd = tid_e & 31;
+  // thread: rows tid / 32 (+ 8, 16, 24), dims 4 (tid % 32) .. +3
+  const int qd = tid_e & 31, r_first = tid_e >> 5;
+  const __amdgpu_buffer_rsrc_t prs = part_rsrc(a);
+  auto finish = [&](int r, const f32x4_t& x, float l) __attribute__((always_inline)) {
+    const int q2 = small_div(r, 1.0f / (float)g);
+    const float inv = normalizer(l, vs, row_limit(a, it, q2, it.nk) > 0);
+    store4<true>(a.o + ((int64_t)(it.qbase + q2) * a.H + kvh * g + (r - q2 * g)) * kRowB + 8 * qd, x[0] * inv,
+                 x[1] * inv, x[2] * inv, x[3] * inv);
+  };
+  auto keep = [&](int slot, int r, const f32x4_t& x, float m, float l) __attribute__((always_inline)) {
+    const uint32_t at = (uint32_t)slot * kSlotBytes;
+    part_store4(prs, at + r * (kDh * 4) + qd * 16, x[0], x[1], x[2], x[3]);
+    if (qd == 0) {
+      part_store(prs, at + kStats + r * 4, m);
+      part_store(prs, at + kStats + (kPagedRows + r) * 4, l);
+    }
+  };
+  for (int r = r_first; r < rows; r += 8) {
     float mr = ml[r], lr = 0.0f;
 #pragma unroll
     for (int w = 1; w < 4; ++w) mr = fmaxf(mr, ml[w * kFew + r]);
@@ -617,19 +733,55 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
       lr = fmaf(ml[(4 + w) * kFew + r], weight(ml[w * kFew + r], mr, c2), lr);
       x += *reinterpret_cast<const f32x4_t*>(ob + (w * kFew + r) * kOLd + 4 * qd);
     }
-    if (partial) {
-      float* const p = part_of(a, it);
-      *reinterpret_cast<f32x4_t*>(p + part_offset(true, r, qd)) = x;
-      if (qd == 0) {
-        p[kPagedRows * kDh + r] = mr;
-        p[kPagedRows * kDh + kPagedRows + r] = lr;
+    if (it.n_chunks > 1)
+      keep(it.slot + it.c, r, x, mr, lr);
+    else
+      finish(r, x, lr);
+  }
+  // ---- the chunks meet, 16 at a time ----
+  int n = it.n_chunks, idx = it.c, stride = 1;
+  for (int level = 0; n > 1; ++level) {
+    const int first = idx / kMeet * kMeet, size = min(kMeet, n - first);
+    const int slot = it.slot + first * stride;
+    if (size > 1 && !arrive_last(a, level * kPagedTarget + slot, size, reinterpret_cast<int*>(ml))) return;
+    n = (n + kMeet - 1) / kMeet;
+    idx /= kMeet;
+    if (size > 1)
+      for (int r = r_first; r < rows; r += 8) {
+        float m = -__builtin_inff(), l = 0.0f;
+        f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int c0 = 0; c0 < size; c0 += 8) {
+          float mc[8], lc[8];
+          f32x4_t y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t at = (uint32_t)(slot + min(c0 + i, size - 1) * stride) * kSlotBytes;
+            mc[i] = part_load(prs, at + kStats + r * 4);
+            lc[i] = part_load(prs, at + kStats + (kPagedRows + r) * 4);
+            y[i] = part_load4(prs, at + r * (kDh * 4) + qd * 16);
+          }
+          float m_new = m;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, mc[i]);
+          const float al = weight(m, m_new, c2);
+          l *= al;
+          x *= al;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (c0 + i < size) {
+              const float wi = weight(mc[i], m_new, c2);
+              l = fmaf(lc[i], wi, l);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = fmaf(y[i][e], wi, x[e]);
+            }
+          m = m_new;
+        }
+        if (n > 1)
+          keep(slot, r, x, m, l);
+        else
+          finish(r, x, l);
       }
-    } else {
-      const int q2 = small_div(r, 1.0f / (float)g);
-      const float inv = normalizer(lr, vs, row_limit(a, it, q2, it.nk) > 0);
-      store4<true>(a.o + ((int64_t)(it.qbase + q2) * a.H + kvh * g + (r - q2 * g)) * kRowB + 8 * qd, x[0] * inv,
-                   x[1] * inv, x[2] * inv, x[3] * inv);
-    }
+    stride *= kMeet;
   }
 }
 
@@ -688,23 +840,29 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   const int q0 = r0 / g;         // first query, and the first row's place in its group
   const int h0 = r0 - q0 * g;
 
-  // ---- page numbers: lane l holds that of this wave's 16 keys of tile tb + l, in
-  //      two windows of 64 tiles ----
+  // ---- page numbers: lane l holds that of this wave's 16 keys of the tile from tb on
+  //      whose number is l modulo 64 ----
   const int32_t* const table = a.table + (int64_t)it.b * a.max_pages;
+  int tb = 0, pages = 0;
   auto load_pages = [&](int tile) __attribute__((always_inline)) {
-    const int64_t key = (int64_t)kbeg + ((int64_t)tile + lane) * kKT + 16 * wave;
-    return key < it.nk ? table[key >> pl] : -1;
+    tb = tile;
+    const int64_t key = (int64_t)kbeg + (int64_t)(tile + ((lane - tile) & 63)) * kKT + 16 * wave;
+    pages = key < it.nk ? table[key >> pl] : -1;
   };
-  int tb = 0;
-  int pages = load_pages(0), pages2 = load_pages(64);
-  auto resource = [&](const char* pool, int tile) __attribute__((always_inline)) {
-    const int i = tile - tb;
-    const int page = i < 64 ? __builtin_amdgcn_readlane(pages, i & 63) : __builtin_amdgcn_readlane(pages2, i & 63);
+  load_pages(0);
+  // where a tile's 16 keys of this wave lie in the pools, and their bytes
+  struct Rows {
+    int64_t at;
+    uint32_t bytes;
+  };
+  auto rows_of = [&](int tile) __attribute__((always_inline)) {
     const int key = kbeg + tile * kKT + 16 * wave;
     bool ok;
-    const int64_t at = page_at<kF8>(a, kvh, page, ok) + (int64_t)(key & mask_p) * kPageRow<kF8>;
-    const int n = ok ? clampi(it.nk - key, 0, 16) : 0;
-    return make_rsrc(pool + at, (uint32_t)(n * kPageRow<kF8>));
+    Rows r;
+    r.at = page_at<kF8>(a, kvh, __builtin_amdgcn_readlane(pages, tile & 63), ok) +
+           (uint32_t)(key & mask_p) * kPageRow<kF8>;
+    r.bytes = ok ? (uint32_t)clampi(it.nk - key, 0, 16) * kPageRow<kF8> : 0;
+    return r;
   };
 
   // ---- K and V tiles: wave w brings rows 16 w .. +15 ----
@@ -716,8 +874,8 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   }
   const uint32_t vvo = opaque((uint32_t)(kr_sub * kRowB + ((kpc ^ (kr_sub << 2)) << 4)));
   u32x4_t kreg[2], vreg[2];  // 8-bit pages: rows 8 i + lane / 8, 16 values lane % 8
-  auto fetch_k = [&](int tile, int buf) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t rs = resource(a.k, tile);
+  auto fetch_k = [&](const Rows& x, int buf) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.k + x.at, x.bytes);
     if constexpr (kF8) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) kreg[i] = bload16(rs, lane * 16 + i * 1024, 0);
@@ -728,8 +886,8 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, region + 4 * i * kRowB, 16, (int)kvo[i], 0, 0, 0);
     }
   };
-  auto fetch_v = [&](int tile, int buf) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t rs = resource(a.v, tile);
+  auto fetch_v = [&](const Rows& x, int buf) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.v + x.at, x.bytes);
     if constexpr (kF8) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) vreg[i] = bload16(rs, lane * 16 + i * 1024, 0);
@@ -894,6 +1052,8 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     f32x16_t sa = f32x16_t{}, sb;
     u32x4_t pa[2], pb[2];
     float ma, mb;
+    const Rows rows0 = rows_of(0);
+    Rows rows1 = rows_of(1);  // of the next V (8-bit: next but one) tile to fetch
     // The wave's 32 rows come by whole-line DMA as well (rows past the end as
     // zeros), chunk c of row r at c ^ (r & 15), into the parts of the two V
     // buffers that this wave itself fills later.
@@ -914,16 +1074,13 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
         __builtin_amdgcn_raw_ptr_buffer_load_lds(qrs, ring + qb + (i >> 2) * kKBytes + 4 * (i & 3) * kRowB, 16, (int)vo, 0,
                                                  0, 0);
       }
-      if constexpr (!kF8) {
-        fetch_k(0, 0);
-        if (ntiles > 1) {
-          fetch_k(1, 1);
-          wait_vmcnt<8>();
-        } else {
-          wait_vmcnt<4>();
-        }
+      fetch_k(rows0, 0);
+      if (!kF8 && ntiles > 1) {
+        fetch_k(rows1, 1);
+        wait_vmcnt<8>();
+      } else if (!kF8) {
+        wait_vmcnt<4>();
       } else {
-        fetch_k(0, 0);
         wait_vmcnt<0>();  // (loads to registers may be issued before the DMAs)
       }
       asm volatile("" ::: "memory");
@@ -935,18 +1092,17 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     }
     if constexpr (kF8) {
       put(kreg, 0, true);
+      fetch_v(rows0, 0);
       if (ntiles > 1) {
-        fetch_k(1, 1);
-        fetch_v(0, 0);
+        fetch_k(rows1, 0);
         put(kreg, kKBytes, true);
-      } else {
-        fetch_v(0, 0);
       }
       put(vreg, 2 * kKBytes, false);
-      if (ntiles > 2) fetch_k(2, 0);
-      if (ntiles > 1) fetch_v(1, 1);
+      if (ntiles > 1) fetch_v(rows1, 0);
+      rows1 = rows_of(2);
+      if (ntiles > 2) fetch_k(rows1, 0);
     } else {
-      fetch_v(0, 0);
+      fetch_v(rows0, 0);
       wait_vmcnt<4>();  // K
     }
     __syncthreads();
@@ -958,26 +1114,24 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     if constexpr (!kF8) wait_vmcnt<0>();
     __syncthreads();  // every wave has read K of tile 0; V of tile 0 is there
     for (int t = 0; t + 1 < ntiles; ++t) {
-      if (t + 1 - tb >= 64) {  // K is fetched up to two (8-bit: three) tiles ahead, V one (two)
-        tb += 64;
-        pages = pages2;
-        pages2 = load_pages(tb + 64);
-      }
+      const Rows ahead = rows_of(kF8 ? t + 3 : t + 2);
       if constexpr (kF8) {
         if (t + 2 < ntiles) put(kreg, (t & 1) * kKBytes, true);
         put(vreg, (2 + ((t + 1) & 1)) * kKBytes, false);
-        if (t + 3 < ntiles) fetch_k(t + 3, 0);
-        if (t + 2 < ntiles) fetch_v(t + 2, 0);
+        if (t + 3 < ntiles) fetch_k(ahead, 0);
+        if (t + 2 < ntiles) fetch_v(rows1, 0);
       } else {
-        if (t + 2 < ntiles) fetch_k(t + 2, t & 1);
+        if (t + 2 < ntiles) fetch_k(ahead, t & 1);
       }
 #pragma unroll
       for (int s2 = 0; s2 < 8; ++s2) koff[s2] ^= kKBytes;
       stage(Half1{}, No{}, No{}, 2 * t + 1, sb, sa, pa, pb, mb, ma);
-      if constexpr (!kF8) fetch_v(t + 1, (t + 1) & 1);
+      if constexpr (!kF8) fetch_v(rows1, (t + 1) & 1);
+      rows1 = ahead;
       stage(Half0{}, No{}, No{}, 2 * t + 2, sa, sb, pb, pa, ma, mb);
 #pragma unroll
       for (int db = 0; db < 4; ++db) voff[db] ^= kKBytes;
+      if (t + 4 - tb >= 64) load_pages(t + 1);  // (the next iteration looks three tiles on)
       if constexpr (!kF8) {
         wait_vmcnt<0>();
         __syncthreads();
@@ -994,20 +1148,64 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   }
 
   l_run += __shfl_xor(l_run, 32);
-  if (it.tile_chunks > 1) {
-    // ---- partial results, as the lanes hold them ----
-    float* const p = part_of(a, it);
+  if (it.n_chunks > 1) {
+    // ---- the chunks meet, 8 at a time; partial results as the lanes hold them ----
+    const __amdgpu_buffer_rsrc_t prs = part_rsrc(a);
+    const uint32_t mine = (uint32_t)(wave * 16 * 64 + lane) * 16;
+    const uint32_t stat = kStats + (uint32_t)(32 * wave + lrow) * 4;
+    int n = it.n_chunks, idx = it.c, stride = 1;
+    int slot = it.slot + it.c;
+    for (int level = 0;; ++level) {
+      {
+        const uint32_t at = (uint32_t)slot * kSlotBytes;
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+        for (int v = 0; v < 16; ++v)
+          part_store4(prs, at + mine + v * 1024, oacc[v >> 2][4 * (v & 3)], oacc[v >> 2][4 * (v & 3) + 1],
+                      oacc[v >> 2][4 * (v & 3) + 2], oacc[v >> 2][4 * (v & 3) + 3]);
+        if (lhalf == 0) {
+          part_store(prs, at + stat, m_run);
+          part_store(prs, at + stat + kPagedRows * 4, l_run);
+        }
+      }
+      int size;
+      for (;; ++level) {
+        const int first = idx / kMeetTile * kMeetTile;
+        size = min(kMeetTile, n - first);
+        slot = it.slot + first * stride;
+        if (size > 1) break;  // (a group of one goes on as it is)
+        n = (n + kMeetTile - 1) / kMeetTile;
+        idx /= kMeetTile;
+        stride *= kMeetTile;
+      }
+      if (!arrive_last(a, level * kPagedTarget + slot, size, reinterpret_cast<int*>(smem + 4 * kFew * kOLd * 4))) return;
+      float mc[kMeetTile];
+      m_run = -__builtin_inff();
 #pragma unroll
-      for (int g4 = 0; g4 < 4; ++g4)
-        *reinterpret_cast<f32x4_t*>(p + ((wave * 16 + 4 * db + g4) * 64 + lane) * 4) =
-            f32x4_t{oacc[db][4 * g4], oacc[db][4 * g4 + 1], oacc[db][4 * g4 + 2], oacc[db][4 * g4 + 3]};
-    if (lhalf == 0) {
-      p[kPagedRows * kDh + 32 * wave + lrow] = m_run;
-      p[kPagedRows * kDh + kPagedRows + 32 * wave + lrow] = l_run;
+      for (int i = 0; i < kMeetTile; ++i) {
+        mc[i] = part_load(prs, (uint32_t)(slot + min(i, size - 1) * stride) * kSlotBytes + stat);
+        m_run = fmaxf(m_run, mc[i]);
+      }
+      l_run = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
+#pragma unroll
+      for (int i = 0; i < kMeetTile; ++i)
+        if (i < size) {
+          const uint32_t at = (uint32_t)(slot + i * stride) * kSlotBytes;
+          const float wi = weight(mc[i], m_run, c2);
+          l_run = fmaf(part_load(prs, at + stat + kPagedRows * 4), wi, l_run);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const f32x4_t y = part_load4(prs, at + mine + v * 1024);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) oacc[v >> 2][4 * (v & 3) + e] = fmaf(y[e], wi, oacc[v >> 2][4 * (v & 3) + e]);
+          }
+        }
+      n = (n + kMeetTile - 1) / kMeetTile;
+      idx /= kMeetTile;
+      stride *= kMeetTile;
+      if (n == 1) break;
     }
-    return;
   }
   // ---- O = O^T / l, turned through LDS into whole rows (256 bytes by 16 lanes).
   //      The wave uses its own 8 KB of the K buffers, which no wave reads after
