@@ -34,9 +34,10 @@ struct AppendArgs {
   const float *k_scale, *v_scale;
 };
 
-// Items and partial results of the sequences before one, and its units that are not cut.
+// Items, partial results and cut units of the sequences before one, and its units
+// that are not cut.
 struct PagedPlan {
-  uint32_t items, slots, whole;
+  uint32_t items, slots, cut, whole;
 };
 
 struct PagedArgs {
@@ -49,6 +50,7 @@ struct PagedArgs {
   int64_t page_bytes;  // bytes between pages
   int B, H, Hkv, q_cap, n_pages, max_pages, page_log2, causal;
   float scale_log2;  // scale * log2(e)
+  int meet_in_launch;  // the chunks of a unit meet in the launch itself
   uint32_t grid;     // items that the launch has workgroups for
   float* part;       // partial results, kPagedPart floats a slot
   unsigned long long* arrived;  // counters of the chunks that meet, kPagedTarget a level
@@ -61,11 +63,13 @@ constexpr int kPagedTarget = 512;  // places for workgroups: two on each CU
 constexpr int kPagedRows = 128;    // (query, head) rows of a tile
 constexpr int kPagedPart = kPagedRows * (128 + 2);  // floats of a slot: outputs, maxima, sums
 
-constexpr int kPagedLevels = 3;     // eight or sixteen chunks meet at a time, 512 at most
+constexpr int kPagedLevels = 3;    // sixteen chunks meet at a time, 512 at most
 
 // What the host knows of a call: the workgroups that any batch of these sizes needs.
 struct PagedGrid {
   int64_t items;
+  int meet_in_launch;
+  int cut_units;  // for the launch that adds chunks up, at most (0: no such launch)
   size_t plan_bytes, count_bytes, bytes;  // workspace: the plan, arrival counters, partial results
 };
 PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys);

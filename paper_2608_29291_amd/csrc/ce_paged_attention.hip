@@ -18,8 +18,7 @@
 // (the plan: ce_paged_tile.hpp). Every wave forms the plan by itself from the
 // lengths, which only the device knows: a lane per sequence, or per four, and a few
 // prefix sums; more than 256 sequences are planned by a launch of their own. The
-// chunks of a cut tile meet through the workspace, where the last to arrive adds them
-// up in order, so one launch does it all and no result depends on which
+// chunks of a cut tile are added up in chunk order, so no result depends on which
 // workgroup came first.
 //
 // A key that a query does not see has no influence: its score is replaced before
@@ -50,7 +49,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int in_xcd = w / kXcdCount;
   const uint32_t at = (in_xcd / group) * (kXcdCount * group) + (w % kXcdCount) * group + in_xcd % group;
   Item it;
-  if (!find_item(a, at, it)) return;
+  if (!find_item<false>(a, at, it)) return;
   if (it.few)
     paged_few<kF8>(a, smem, it);
   else
@@ -58,10 +57,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // The plan of more than kPagedScan sequences. One workgroup.
-__global__ __launch_bounds__(1024) void paged_plan_kernel(PagedArgs a) {
-  __shared__ int64_t scr[16];
-  __shared__ float wsum[16];
-  __shared__ int wmax[16];
+__global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
+  __shared__ int64_t scr[8];
+  __shared__ float wsum[8];
+  __shared__ float wmax[8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = a.H / a.Hkv;
   // exclusive prefix sum over the threads, and the total
@@ -77,7 +76,7 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedArgs a) {
     __syncthreads();
     int64_t before = 0;
     total = 0;
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 8; ++i) {
       if (i < wave) before += scr[i];
       total += scr[i];
     }
@@ -89,63 +88,139 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedArgs a) {
     if (lane == 0) wsum[wave] = v;
     __syncthreads();
     float s = 0.0f;
-    for (int i = 0; i < 16; ++i) s += wsum[i];
+    for (int i = 0; i < 8; ++i) s += wsum[i];
     return s;
   };
-  float w = 0.0f;
-  int longest = 0;
+  float w = 0.0f, most = 0.0f;
   int64_t units = 0, total;
-  for (int b = tid; b < a.B; b += 1024) {
+  for (int b = tid; b < a.B; b += 512) {
     const Size s = size_of(a, b, g);
     const uint32_t n = (uint32_t)s.tiles * a.Hkv;
-    w += (float)n * (float)s.nk;
+    const float c = n ? cost_of(s, g) : 0.0f;
+    w += (float)n * c;
     units += n;
-    longest = max(longest, n ? s.nk : 0);
+    most = fmaxf(most, c);
   }
   w = sum(w);
-  longest = wave_max(longest);
-  if (lane == 0) wmax[wave] = longest;
+  most = wave_max(most);
+  if (lane == 0) wmax[wave] = most;
   scan(units, total);  // (its barriers stand between)
-  for (int i = 0; i < 16; ++i) longest = max(longest, wmax[i]);
-  uint32_t whole = whole_units((uint32_t)min(total, (int64_t)1 << 30), w, longest);
-  // the units before each sequence, and the rest's keys
+  for (int i = 0; i < 8; ++i) most = fmaxf(most, wmax[i]);
+  const uint32_t whole = whole_units((uint32_t)min(total, (int64_t)1 << 30), w, most);
+  // the units before each sequence, and what the rest costs
   float rest = 0.0f;
   int64_t base = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 1024) {
+  for (int b0 = 0; b0 < a.B; b0 += 512) {
     const int b = b0 + tid;
     Size s = {0, 0, 0, 0};
     if (b < a.B) s = size_of(a, b, g);
     const uint32_t n = (uint32_t)s.tiles * a.Hkv;
     const int64_t first = base + scan(n, total);
     const uint32_t wh = whole_of(a, s, (uint32_t)min(first, (int64_t)1 << 30), whole);
-    rest += (float)(n - wh) * (float)s.nk;
+    rest += (float)(n - wh) * cost_of(s, g);
     if (b < a.B) a.plan[b].whole = wh;
     base += total;
   }
   if (whole) w = sum(rest);
   int L = chunk_length(w);
   for (;;) {
-    int64_t items = 0, slots = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 1024) {
+    int64_t items = 0, slots = 0, cuts = 0;
+    auto put = [](int64_t x) { return (uint32_t)min(x, (int64_t)1 << 30); };
+    for (int b0 = 0; b0 < a.B; b0 += 512) {
       const int b = b0 + tid;
-      uint32_t ni = 0, ns = 0;
-      if (b < a.B) counts_of(a, size_of(a, b, g), g, L, a.plan[b].whole, ni, ns);
-      const int64_t i0 = items + scan(ni, total);
+      Counts c = {0, 0, 0};
+      if (b < a.B) c = counts_of(a, size_of(a, b, g), g, L, a.plan[b].whole);
+      const int64_t i0 = items + scan(c.items, total);
       items += total;
-      const int64_t s0 = slots + scan(ns, total);
+      const int64_t s0 = slots + scan(c.slots, total);
       slots += total;
+      const int64_t c0 = cuts + scan(c.cut, total);
+      cuts += total;
       if (b < a.B) {
-        a.plan[b].items = (uint32_t)min(i0, (int64_t)1 << 30);
-        a.plan[b].slots = (uint32_t)min(s0, (int64_t)1 << 30);
+        a.plan[b].items = put(i0);
+        a.plan[b].slots = put(s0);
+        a.plan[b].cut = put(c0);
       }
     }
     if (tid == 0) {
-      a.plan[a.B].items = (uint32_t)min(items, (int64_t)1 << 30);
+      a.plan[a.B].items = put(items);
+      a.plan[a.B].cut = put(cuts);
       a.plan[a.B].whole = (uint32_t)L;
     }
     // (as in find_by_scan)
     if (L == 1 << 30 || (items <= a.grid && slots <= kPagedTarget)) break;
     L = 1 << 30;
+  }
+}
+
+// Partial results of the cut units, in chunk order. Workgroup (unit, z): 32 rows z of
+// a 128-row tile, as wave z of its chunks' workgroups left them; of a few rows, eight.
+__global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
+  Item it;
+  if (!find_item<true>(a, blockIdx.x, it) || it.n_chunks <= 1) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int g = a.H / a.Hkv;
+  const int n = it.n_chunks;
+  const float c2 = a.scale_log2 * (a.ks ? a.ks[it.kvh] : 1.0f);
+  const float vs = a.vs ? a.vs[it.kvh] : 1.0f;
+  const float* const slot = a.part + (int64_t)it.slot * kPagedPart;
+  auto add = [&](auto n_c, auto batch_c, const float* p, int step, int r, auto out) __attribute__((always_inline)) {
+    constexpr int kN = decltype(n_c)::value, kBatch = decltype(batch_c)::value;
+    const float* const ps = slot + kPagedRows * kDh + r;
+    float m = -__builtin_inff(), l = 0.0f;
+    f32x4_t x[kN];
+#pragma unroll
+    for (int v = 0; v < kN; ++v) x[v] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c0 = 0; c0 < n; c0 += kBatch) {
+      float mc[kBatch], lc[kBatch];
+      f32x4_t y[kBatch][kN];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int64_t at = (int64_t)min(c0 + i, n - 1) * kPagedPart;
+        mc[i] = ps[at];
+        lc[i] = ps[at + kPagedRows];
+#pragma unroll
+        for (int v = 0; v < kN; ++v) y[i][v] = *reinterpret_cast<const f32x4_t*>(p + at + v * step);
+      }
+      float m_new = m;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) m_new = fmaxf(m_new, mc[i]);
+      const float al = weight(m, m_new, c2);
+      l *= al;
+#pragma unroll
+      for (int v = 0; v < kN; ++v) x[v] *= al;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (c0 + i < n) {
+          const float wi = weight(mc[i], m_new, c2);
+          l = fmaf(lc[i], wi, l);
+#pragma unroll
+          for (int v = 0; v < kN; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[v][e] = fmaf(y[i][v][e], wi, x[v][e]);
+        }
+      m = m_new;
+    }
+    if (r >= it.rows) return;
+    const int row = it.tile * kPagedRows + r;
+    const int qi = row / g;
+    const float inv = normalizer(l, vs, row_limit(a, it, qi, it.nk) > 0);
+    char* const o = a.o + ((int64_t)(it.qbase + qi) * a.H + it.kvh * g + (row - qi * g)) * kRowB;
+#pragma unroll
+    for (int v = 0; v < kN; ++v) store4<true>(o + 2 * out(v), x[v][0] * inv, x[v][1] * inv, x[v][2] * inv, x[v][3] * inv);
+  };
+  using One = std::integral_constant<int, 1>;
+  using Four = std::integral_constant<int, 4>;
+  if (it.few) {
+    for (int rb = 8 * blockIdx.y; rb < it.rows; rb += 8 * gridDim.y) {
+      const int r = rb + (tid >> 5), d = 4 * (tid & 31);
+      const int at = min(r, it.rows - 1) * kDh + d;
+      add(One{}, std::integral_constant<int, 16>{}, slot + at, 0, r, [&](int) { return d; });
+    }
+  } else {
+    for (int z = blockIdx.y; z < 4 && 32 * z < it.rows; z += gridDim.y)  // accumulators 4 wave .. +3 of wave z
+      add(Four{}, Four{}, slot + ((z * 16 + 4 * wave) * 64 + lane) * 4, 256, 32 * z + (lane & 31),
+          [&](int v) { return 32 * wave + 8 * v + 4 * (lane >> 5); });
   }
 }
 
@@ -170,8 +245,13 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
   p.items = ((int64_t)q_cap * (H / Hkv) / kPagedRows + (B < q_cap ? B : q_cap)) * Hkv;
   if (B > kPagedScan) p.plan_bytes = ((size_t)(B + 1) * sizeof(PagedPlan) + 255) / 256 * 256;
   p.bytes = p.plan_bytes;
-  if (max_keys >= 2 * kMinChunk) {  // else nothing is cut
+  if (max_keys >= 2 * kMinFew) {  // else nothing is cut
     p.items += kPagedTarget;
+    // Chunks meet in the launch itself where there are no more rows than a thread for
+    // each 16 bytes of a chunk's outputs can take at once: single tokens.
+    p.meet_in_launch = q_cap <= B && H / Hkv <= 8;
+    const int64_t units = ((int64_t)q_cap * (H / Hkv) / kPagedRows + (B < q_cap ? B : q_cap)) * Hkv;
+    if (!p.meet_in_launch) p.cut_units = (int)(units < kPagedTarget / 2 ? units : kPagedTarget / 2);
     p.count_bytes = (size_t)kPagedLevels * kPagedTarget * sizeof(unsigned long long);
     p.bytes += p.count_bytes + (size_t)kPagedTarget * kPagedPart * sizeof(float);
   }
@@ -186,9 +266,10 @@ hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
   const int64_t unit = (int64_t)kXcdCount * group;
   const int64_t grid = (p.items + unit - 1) / unit * unit;
   a.grid = (uint32_t)grid;
+  a.meet_in_launch = p.meet_in_launch;
   a.token = paged_token();
   if (a.B > kPagedScan) {
-    hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, stream, a);
+    hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(512), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -196,6 +277,9 @@ hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
     hipLaunchKernelGGL(paged_attention_kernel<true>, dim3((unsigned)grid), dim3(256), 0, stream, a, group);
   else
     hipLaunchKernelGGL(paged_attention_kernel<false>, dim3((unsigned)grid), dim3(256), 0, stream, a, group);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.cut_units == 0) return e;
+  hipLaunchKernelGGL(paged_combine_kernel, dim3(p.cut_units, 4), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

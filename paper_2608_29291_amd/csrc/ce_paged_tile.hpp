@@ -19,9 +19,9 @@ constexpr int kBK = 32;            // keys per block: one pass of the softmax
 constexpr int kKBytes = kKT * kRowB;
 constexpr int kAhead = 3;          // MFMA operands read from LDS this many products ahead
 constexpr float kLazy = 8.0f;      // headroom of the running maximum (exponent of 2)
-constexpr int kMinChunk = 256;     // least keys of a chunk
-constexpr int kMeet = 16;          // chunks that meet at a time: paged_few
-constexpr int kMeetTile = 8;       // and paged_tile
+constexpr int kMinFew = 128;       // least keys of a chunk: one tile of 32 for each wave
+constexpr int kMinTile = 256;
+constexpr int kMeet = 16;          // chunks that meet at a time in the launch itself
 constexpr int kOLd = kDh + 4;      // floats per row of paged_few's outputs in LDS
 constexpr int kVRow = kBK * 2;     // bytes per row of paged_few's V^T
 constexpr int kVTile = kDh * kVRow;
@@ -34,8 +34,9 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 //
 // A unit is a row tile of a sequence for one key/value head; units are numbered
 // sequence by sequence, head by head, the last tiles first (under a causal mask they
-// see the most keys). With S = 512 places for workgroups (two on each CU) and
-// A = (sum of the units' keys) / S:
+// see the most keys). A key costs a tile of 128 rows about twice what it costs a few
+// rows, so keys are counted as 1 and 1/2. With S = 512 places for workgroups (two on
+// each CU) and A = (sum of the units' keys) / S:
 //   * a batch of many units fills S places some whole number of times and leaves
 //     a rest; the units before the rest are whole, and the rest, fewer than S, are cut
 //     along their keys so that they too fill the places: L = (their keys) / S;
@@ -44,6 +45,11 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 // A unit of n_k keys is cut into floor(n_k / L) chunks, so the chunks of all cut units
 // are at most S (a second round of a few would double the time) and as many
 // partial results fit the workspace.
+//
+// How the chunks meet: of a few rows, in the launch itself (a second one would cost
+// 5 us of 18); of many rows, by a second launch over the whole chip, since one
+// workgroup would read 64 KB a chunk (a.meet_in_launch, from the host: then only
+// the few-row units are cut).
 
 struct Size {
   int qbase, nq, nk, tiles;
@@ -64,23 +70,25 @@ __device__ __forceinline__ Size size_of(const PagedArgs& a, int b, int g) {
   return size_from(a, a.qo[b], a.qo[b + 1], a.lens[b], g);
 }
 
-// Units before the rest, of n in all with w keys, the longest of which has `longest`.
-__device__ __forceinline__ uint32_t whole_units(uint32_t n, float w, int longest) {
-  return (float)longest * (0.5f * kPagedTarget) >= w ? 0 : n / kPagedTarget * kPagedTarget;
+// Units before the rest, of n in all that cost w, the dearest `most`.
+__device__ __forceinline__ uint32_t whole_units(uint32_t n, float w, float most) {
+  return most * (0.5f * kPagedTarget) >= w ? 0 : n / kPagedTarget * kPagedTarget;
 }
 
 // Keys per chunk where the units that may be cut have w keys.
 __device__ __forceinline__ int chunk_length(float w) {
   const float l = w * (1.0f / kPagedTarget);
-  return l < (float)kMinChunk ? kMinChunk : l > 1e9f ? 1 << 30 : (int)l + 1;
+  return l > 1e9f ? 1 << 30 : (int)l + 1;
 }
 
-// A sequence's chunks (a whole number of the tiles that its waves take in turn).
-__device__ __forceinline__ void cut(const Size& s, int g, int L, int& C, int& chunk) {
-  C = s.nk / L;
+// A sequence's chunks (a whole number of its waves' tiles).
+__device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, int& C, int& chunk) {
+  const bool few = is_few(s.nq, g);
+  C = s.nk / (few ? max(2 * min(L, 1 << 29), kMinFew) : max(L, kMinTile));
+  if (!few && a.meet_in_launch) C = 1;
   chunk = s.nk;
   if (C > 1) {
-    const int unit = is_few(s.nq, g) ? 4 * kBK : kKT;
+    const int unit = few ? kBK : kKT;
     chunk = (int)(((uint32_t)s.nk + C - 1) / (uint32_t)C + unit - 1) / unit * unit;
     C = (int)(((uint32_t)s.nk + chunk - 1) / (uint32_t)chunk);
   }
@@ -96,14 +104,24 @@ __device__ __forceinline__ uint32_t whole_of(const PagedArgs& a, const Size& s, 
   return whole <= first ? 0 : min(n, whole - first);
 }
 
-// Its items, and its partial results.
-__device__ __forceinline__ void counts_of(const PagedArgs& a, const Size& s, int g, int L, uint32_t whole, uint32_t& items,
-                                          uint32_t& slots) {
+// Its keys as the plan counts them, per unit.
+__device__ __forceinline__ float cost_of(const Size& s, int g) {
+  return (float)s.nk * (is_few(s.nq, g) ? 0.5f : 1.0f);
+}
+
+// Its items, its partial results and the units that have such.
+struct Counts {
+  uint32_t items, slots, cut;
+};
+__device__ __forceinline__ Counts counts_of(const PagedArgs& a, const Size& s, int g, int L, uint32_t whole) {
   int C, chunk;
-  cut(s, g, L, C, chunk);
+  cut(a, s, g, L, C, chunk);
   const uint32_t n = (uint32_t)s.tiles * a.Hkv;
-  slots = C > 1 ? (n - whole) * C : 0;
-  items = C > 1 ? whole + slots : n;
+  Counts c;
+  c.cut = C > 1 ? n - whole : 0;
+  c.slots = c.cut * C;
+  c.items = C > 1 ? whole + c.slots : n;
+  return c;
 }
 
 struct Item {
@@ -148,93 +166,98 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
-// Largest of non-negative values over the wave.
-__device__ __forceinline__ int wave_max(int v) {
+// Largest of non-negative values over the wave (their bits are in order).
+__device__ __forceinline__ float wave_max(float x) {
+  int v = (int)__float_as_uint(x);
   v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
   v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
   v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
   v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
   v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
   v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
-  return __builtin_amdgcn_readlane(v, 63);
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v, 63));
 }
 
-// The sequence that holds an item, and what was counted before it.
+// The sequence that holds an item (or a cut unit), and what was counted before it.
 struct Found {
   int b, L;
   Size size;
   uint32_t whole;         // its units that stay whole
-  uint32_t items, slots;  // of the sequences before
+  uint32_t before, slots; // items (or cut units) and partial results of the sequences before
 };
 
-// The sequence of item `at`; false past the last. Every wave finds it by itself, kPer
-// sequences a lane.
-template <int kPer>
+// The sequence of item `at` (kCut: of cut unit `at`); false past the last. Every wave
+// finds it by itself, kPer sequences a lane.
+template <int kPer, bool kCut>
 __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t at, Found& f) {
   const int lane = threadIdx.x & 63;
   Size s[kPer];
-  float w = 0.0f;
+  float w = 0.0f, most = 0.0f;
   uint32_t units = 0;
-  int longest = 0;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int b = lane * kPer + i;
     s[i] = Size{0, 0, 0, 0};
     if (b < a.B) s[i] = size_of(a, b, g);
     const uint32_t n = (uint32_t)s[i].tiles * a.Hkv;
-    w += (float)n * (float)s[i].nk;
+    const float c = n ? cost_of(s[i], g) : 0.0f;
+    w += (float)n * c;
     units += n;
-    longest = max(longest, n ? s[i].nk : 0);
+    most = fmaxf(most, c);
   }
   const uint32_t units_to = wave_scan(units);
   w = wave_sum(w);
   const uint32_t all = __builtin_amdgcn_readlane(units_to, 63);
-  uint32_t whole = whole_units(all, w, wave_max(longest));
-  if (whole) {  // the rest's keys
+  const uint32_t whole = all < (uint32_t)kPagedTarget ? 0 : whole_units(all, w, wave_max(most));
+  if (whole) {  // what the rest costs
     float rest = 0.0f;
     uint32_t first = units_to - units;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const uint32_t n = (uint32_t)s[i].tiles * a.Hkv;
-      rest += (float)(n - whole_of(a, s[i], first, whole)) * (float)s[i].nk;
+      rest += (float)(n - whole_of(a, s[i], first, whole)) * cost_of(s[i], g);
       first += n;
     }
     w = wave_sum(rest);
   }
   f.L = chunk_length(w);
-  uint32_t items[kPer], slots[kPer], wh[kPer], sum_i, sum_s, items_to, slots_to;
+  uint32_t count[kPer], slots[kPer], wh[kPer], sum, sum_s, to, slots_to;
   for (;;) {
-    sum_i = sum_s = 0;
-    uint32_t first = units_to - units;
+    uint32_t items = 0, first = units_to - units;
+    sum = sum_s = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       wh[i] = whole_of(a, s[i], first, whole);
-      counts_of(a, s[i], g, f.L, wh[i], items[i], slots[i]);
+      const Counts c = counts_of(a, s[i], g, f.L, wh[i]);
       first += (uint32_t)s[i].tiles * a.Hkv;
-      sum_i += items[i];
+      count[i] = kCut ? c.cut : c.items;
+      slots[i] = c.slots;
+      items += c.items;
+      sum += count[i];
       sum_s += slots[i];
     }
-    items_to = wave_scan(sum_i);
     slots_to = wave_scan(sum_s);
+    to = wave_scan(sum);
+    const uint32_t items_all = __builtin_amdgcn_readlane(kCut ? wave_scan(items) : to, 63);
     // more workgroups than the launch has, or slots than the workspace: only where
     // offsets are out of order. Then nothing is cut (every chunk of a cut unit
     // must run) and what lies past the grid is left.
-    if (f.L == 1 << 30 || (__builtin_amdgcn_readlane(items_to, 63) <= a.grid &&
-                           __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedTarget))
+    if (f.L == 1 << 30 ||
+        (items_all <= a.grid && __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedTarget))
       break;
     f.L = 1 << 30;
   }
-  const uint64_t past = __builtin_amdgcn_ballot_w64(at < items_to);
+  const uint64_t past = __builtin_amdgcn_ballot_w64(at < to);
   if (!past) return false;
   const int ln = __builtin_ctzll(past);
-  f.items = __builtin_amdgcn_readlane(items_to - sum_i, ln);
+  f.before = __builtin_amdgcn_readlane(to - sum, ln);
   f.slots = __builtin_amdgcn_readlane(slots_to - sum_s, ln);
   bool found = false;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const uint32_t ni = __builtin_amdgcn_readlane(items[i], ln);
+    const uint32_t ni = __builtin_amdgcn_readlane(count[i], ln);
     if (found) continue;
-    if (i == kPer - 1 || at < f.items + ni) {
+    if (i == kPer - 1 || at < f.before + ni) {
       found = true;
       f.b = ln * kPer + i;
       f.size.qbase = __builtin_amdgcn_readlane(s[i].qbase, ln);
@@ -243,7 +266,7 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
       f.size.tiles = __builtin_amdgcn_readlane(s[i].tiles, ln);
       f.whole = __builtin_amdgcn_readlane(wh[i], ln);
     } else {
-      f.items += ni;
+      f.before += ni;
       f.slots += __builtin_amdgcn_readlane(slots[i], ln);
     }
   }
@@ -251,22 +274,23 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
 }
 
 // The same from the plan in memory: three rounds of 64 samples.
+template <bool kCut>
 __device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, uint32_t at, Found& f) {
   const int lane = threadIdx.x & 63;
-  if (at >= a.plan[a.B].items) return false;
-  int lo = 0;  // the last sequence whose items begin at or before `at` is in [lo, lo + 64 step)
+  auto key = [&](int b) __attribute__((always_inline)) { return kCut ? a.plan[b].cut : a.plan[b].items; };
+  if (at >= key(a.B)) return false;
+  int lo = 0;  // the last sequence whose count begins at or before `at` is in [lo, lo + 64 step)
 #pragma unroll
   for (int step = 4096; step > 0; step >>= 6) {
     const int i = lo + lane * step;
-    const bool le = i < a.B && a.plan[i < a.B ? i : 0].items <= at;
+    const bool le = i < a.B && key(i < a.B ? i : 0) <= at;
     const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(le));
     lo += (n > 0 ? n - 1 : 0) * step;
   }
   f.b = __builtin_amdgcn_readfirstlane(lo);
-  const PagedPlan p = a.plan[f.b];
-  f.items = __builtin_amdgcn_readfirstlane(p.items);
-  f.slots = __builtin_amdgcn_readfirstlane(p.slots);
-  f.whole = __builtin_amdgcn_readfirstlane(p.whole);
+  f.before = __builtin_amdgcn_readfirstlane(key(f.b));
+  f.slots = __builtin_amdgcn_readfirstlane(a.plan[f.b].slots);
+  f.whole = __builtin_amdgcn_readfirstlane(a.plan[f.b].whole);
   f.L = __builtin_amdgcn_readfirstlane((int)a.plan[a.B].whole);
   const Size s = size_of(a, f.b, g);
   f.size.qbase = __builtin_amdgcn_readfirstlane(s.qbase);
@@ -276,11 +300,15 @@ __device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, uint32_t
   return true;
 }
 
+// Item `at` (kCut: cut unit `at`, as its first chunk); false if there is none, or its
+// rows see no key of it.
+template <bool kCut>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item& it) {
   const int g = a.H / a.Hkv;
   Found f;
-  if (!(a.B <= 64 ? find_by_scan<1>(a, g, at, f)
-                  : a.B <= kPagedScan ? find_by_scan<kPagedScan / 64>(a, g, at, f) : find_in_plan(a, g, at, f)))
+  if (!(a.B <= 64 ? find_by_scan<1, kCut>(a, g, at, f)
+                  : a.B <= kPagedScan ? find_by_scan<kPagedScan / 64, kCut>(a, g, at, f)
+                                      : find_in_plan<kCut>(a, g, at, f)))
     return false;
   it.b = f.b;
   it.qbase = f.size.qbase;
@@ -288,11 +316,14 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item&
   it.nk = f.size.nk;
   it.few = is_few(it.nq, g);
   int C;
-  cut(f.size, g, f.L, C, it.chunk);
-  uint32_t u = at - f.items;
+  cut(a, f.size, g, f.L, C, it.chunk);
+  uint32_t u = at - f.before;
   it.c = 0;
   it.slot = 0;
-  if (C > 1 && u >= f.whole) {
+  if (kCut) {
+    it.slot = (int)(f.slots + u * C);
+    u += f.whole;
+  } else if (C > 1 && u >= f.whole) {
     const uint32_t v = u - f.whole;
     const uint32_t back = v / (uint32_t)C;
     it.c = (int)(v - back * C);
@@ -326,12 +357,12 @@ __device__ __forceinline__ float normalizer(float l, float vs, bool sees) {
   return sees ? vs / l : 0.0f;
 }
 
-// Partial results of the chunks of a unit meet through the workspace. Each chunk's
+// Partial results of the chunks of a unit meet through the workspace, in chunk order,
+// so no result depends on who came first. In the launch itself: each chunk's
 // workgroup writes its own and arrives; the last of a group of neighbours adds the
-// group up in chunk order, so no result depends on who came last, and goes on as one
-// chunk of the next level. Nobody waits for anybody. The sums move by device-coherent
-// (sc1) stores and loads, and a workgroup arrives when its stores have completed, so
-// no cache is written back or dropped.
+// group up and goes on as one chunk of the next level. Nobody waits for anybody. The
+// sums move by device-coherent (sc1) stores and loads, and a workgroup arrives when
+// its stores have completed, so no cache is written back or dropped.
 constexpr int kSC1 = 16;            // cache-policy operand: sc1
 constexpr uint32_t kSlotBytes = kPagedPart * 4;
 constexpr uint32_t kStats = kPagedRows * kDh * 4;  // maxima, then sums, behind a slot's outputs
@@ -354,22 +385,25 @@ __device__ __forceinline__ float part_load(__amdgpu_buffer_rsrc_t rs, uint32_t a
 }
 
 // This workgroup's stores are complete and it arrives at counter `i`: is it the last of
-// n? A counter holds the call's token above the arrivals; any other content, whatever
-// the workspace held before, counts as none, and the last leaves zero (a captured call
-// replays with the same token). `said`: a word of LDS that nobody else uses meanwhile.
+// n? A counter holds the call's token above the arrivals. Any other content, whatever
+// the workspace held before, counts as none: the first to come puts the token there,
+// the last leaves zero (a captured call replays with the same token). One exchange at
+// most, then one addition: sixteen that exchanged until it went well took 8 us.
+// `said`: a word of LDS that nobody else uses meanwhile.
 __device__ __forceinline__ bool arrive_last(const PagedArgs& a, int i, int n, int* said) {
   asm volatile("" ::: "memory");
   wait_vmcnt<0>();
   __syncthreads();
   if (threadIdx.x == 0) {
     unsigned long long* const p = a.arrived + i;
-    unsigned long long old = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), next;
-    do {
-      next = (old >> 16) == a.token ? old + 1 : (a.token << 16) + 1;
-      if ((int)(next & 0xffff) == n) next = 0;
-    } while (!__hip_atomic_compare_exchange_strong(p, &old, next, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT));
-    *said = next == 0;
+    unsigned long long was = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool first = (was >> 16) != a.token &&
+                       __hip_atomic_compare_exchange_strong(p, &was, (a.token << 16) + 1, __ATOMIC_RELAXED,
+                                                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!first) was = __hip_atomic_fetch_add(p, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool last = !first && (int)(was & 0xffff) == n - 1;
+    if (last) __hip_atomic_store(p, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *said = last;
   }
   __syncthreads();
   const bool last = __builtin_amdgcn_readfirstlane(*said) != 0;
@@ -738,49 +772,50 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     else
       finish(r, x, lr);
   }
-  // ---- the chunks meet, 16 at a time ----
+  if (!a.meet_in_launch) return;
+  // ---- the chunks meet, 16 at a time, eight rows at a time; all their loads are in
+  //      flight together ----
   int n = it.n_chunks, idx = it.c, stride = 1;
   for (int level = 0; n > 1; ++level) {
     const int first = idx / kMeet * kMeet, size = min(kMeet, n - first);
     const int slot = it.slot + first * stride;
-    if (size > 1 && !arrive_last(a, level * kPagedTarget + slot, size, reinterpret_cast<int*>(ml))) return;
     n = (n + kMeet - 1) / kMeet;
     idx /= kMeet;
-    if (size > 1)
-      for (int r = r_first; r < rows; r += 8) {
-        float m = -__builtin_inff(), l = 0.0f;
-        f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int c0 = 0; c0 < size; c0 += 8) {
-          float mc[8], lc[8];
-          f32x4_t y[8];
+    if (size > 1) {
+      if (!arrive_last(a, level * kPagedTarget + slot, size, reinterpret_cast<int*>(ml))) return;
+      int slot_v = slot;
+      asm volatile("" : "+v"(slot_v));  // (sixteen offsets in scalar registers are too many)
+      for (int rb = 0; rb < rows; rb += 8) {
+        const int r = min(rb + r_first, rows - 1);
+        f32x4_t y[kMeet];
+        float mc[kMeet], lc[kMeet];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t at = (uint32_t)(slot + min(c0 + i, size - 1) * stride) * kSlotBytes;
-            mc[i] = part_load(prs, at + kStats + r * 4);
-            lc[i] = part_load(prs, at + kStats + (kPagedRows + r) * 4);
-            y[i] = part_load4(prs, at + r * (kDh * 4) + qd * 16);
-          }
-          float m_new = m;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, mc[i]);
-          const float al = weight(m, m_new, c2);
-          l *= al;
-          x *= al;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (c0 + i < size) {
-              const float wi = weight(mc[i], m_new, c2);
-              l = fmaf(lc[i], wi, l);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = fmaf(y[i][e], wi, x[e]);
-            }
-          m = m_new;
+        for (int i = 0; i < kMeet; ++i) {
+          const uint32_t at = (uint32_t)(slot_v + min(i, size - 1) * stride) * kSlotBytes;
+          y[i] = part_load4(prs, at + r * (kDh * 4) + qd * 16);
+          mc[i] = part_load(prs, at + kStats + r * 4);
+          lc[i] = part_load(prs, at + kStats + (kPagedRows + r) * 4);
         }
-        if (n > 1)
-          keep(slot, r, x, m, l);
-        else
-          finish(r, x, l);
+        f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+        float m = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMeet; ++i) m = fmaxf(m, mc[i]);
+#pragma unroll
+        for (int i = 0; i < kMeet; ++i)
+          if (i < size) {
+            const float wi = weight(mc[i], m, c2);
+            l = fmaf(lc[i], wi, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = fmaf(y[i][e], wi, x[e]);
+          }
+        if (rb + r_first < rows) {
+          if (n > 1)
+            keep(slot, r, x, m, l);
+          else
+            finish(r, x, l);
+        }
       }
+    }
     stride *= kMeet;
   }
 }
@@ -1149,63 +1184,18 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
 
   l_run += __shfl_xor(l_run, 32);
   if (it.n_chunks > 1) {
-    // ---- the chunks meet, 8 at a time; partial results as the lanes hold them ----
-    const __amdgpu_buffer_rsrc_t prs = part_rsrc(a);
-    const uint32_t mine = (uint32_t)(wave * 16 * 64 + lane) * 16;
-    const uint32_t stat = kStats + (uint32_t)(32 * wave + lrow) * 4;
-    int n = it.n_chunks, idx = it.c, stride = 1;
-    int slot = it.slot + it.c;
-    for (int level = 0;; ++level) {
-      {
-        const uint32_t at = (uint32_t)slot * kSlotBytes;
+    // ---- partial results, as the lanes hold them, for paged_combine_kernel ----
+    float* const p = a.part + (int64_t)(it.slot + it.c) * kPagedPart;
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          part_store4(prs, at + mine + v * 1024, oacc[v >> 2][4 * (v & 3)], oacc[v >> 2][4 * (v & 3) + 1],
-                      oacc[v >> 2][4 * (v & 3) + 2], oacc[v >> 2][4 * (v & 3) + 3]);
-        if (lhalf == 0) {
-          part_store(prs, at + stat, m_run);
-          part_store(prs, at + stat + kPagedRows * 4, l_run);
-        }
-      }
-      int size;
-      for (;; ++level) {
-        const int first = idx / kMeetTile * kMeetTile;
-        size = min(kMeetTile, n - first);
-        slot = it.slot + first * stride;
-        if (size > 1) break;  // (a group of one goes on as it is)
-        n = (n + kMeetTile - 1) / kMeetTile;
-        idx /= kMeetTile;
-        stride *= kMeetTile;
-      }
-      if (!arrive_last(a, level * kPagedTarget + slot, size, reinterpret_cast<int*>(smem + 4 * kFew * kOLd * 4))) return;
-      float mc[kMeetTile];
-      m_run = -__builtin_inff();
-#pragma unroll
-      for (int i = 0; i < kMeetTile; ++i) {
-        mc[i] = part_load(prs, (uint32_t)(slot + min(i, size - 1) * stride) * kSlotBytes + stat);
-        m_run = fmaxf(m_run, mc[i]);
-      }
-      l_run = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
-#pragma unroll
-      for (int i = 0; i < kMeetTile; ++i)
-        if (i < size) {
-          const uint32_t at = (uint32_t)(slot + i * stride) * kSlotBytes;
-          const float wi = weight(mc[i], m_run, c2);
-          l_run = fmaf(part_load(prs, at + stat + kPagedRows * 4), wi, l_run);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const f32x4_t y = part_load4(prs, at + mine + v * 1024);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) oacc[v >> 2][4 * (v & 3) + e] = fmaf(y[e], wi, oacc[v >> 2][4 * (v & 3) + e]);
-          }
-        }
-      n = (n + kMeetTile - 1) / kMeetTile;
-      idx /= kMeetTile;
-      stride *= kMeetTile;
-      if (n == 1) break;
+    for (int v = 0; v < 16; ++v)
+      *reinterpret_cast<f32x4_t*>(p + ((wave * 16 + v) * 64 + lane) * 4) =
+          f32x4_t{oacc[v >> 2][4 * (v & 3)], oacc[v >> 2][4 * (v & 3) + 1], oacc[v >> 2][4 * (v & 3) + 2],
+                  oacc[v >> 2][4 * (v & 3) + 3]};
+    if (lhalf == 0) {
+      p[kPagedRows * kDh + 32 * wave + lrow] = m_run;
+      p[kPagedRows * kDh + kPagedRows + 32 * wave + lrow] = l_run;
     }
+    return;
   }
   // ---- O = O^T / l, turned through LDS into whole rows (256 bytes by 16 lanes).
   //      The wave uses its own 8 KB of the K buffers, which no wave reads after
