@@ -513,13 +513,17 @@ __device__ __forceinline__ uint32_t vt_off(int d, uint32_t u) {
 
 // Up to 32 rows against a chunk of keys: the rows are the columns of one MFMA
 // operand, the 4 waves take tiles of 32 keys in turn and share nothing until the
-// end. K goes from memory to registers in operand order, V through registers
-// (8-bit values converted, exactly, on the way) and a wave-private LDS tile that
-// transposes it; the next tile's loads are issued as soon as the registers are
-// free. Bound: memory.
+// end. Bound: memory, so a wave keeps its next tile's keys and values in flight.
+//   * bf16: whole lines by DMA into LDS of the wave's own, in the layout of
+//     paged_tile; a tile's fragments are read into registers at once, and the next
+//     tile's DMA takes their place. (Fragments loaded straight from memory read a line
+//     of 128 bytes in four instructions, and the line is gone from the cache between
+//     them: 65537 keys 36 us, by DMA see below.)
+//   * 8-bit: K straight to registers in operand order (a line in four loads as well,
+//     but half the bytes: at the copy rate for long caches), V through
+//     registers, converted, exactly, and stored transposed in LDS.
 template <bool kF8>
 __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, const Item& it) {
-  constexpr int kN = kF8 ? 4 : 8;  // 16-byte loads of K, and of V, per lane and tile
   float* const ml = reinterpret_cast<float*>(smem + 4 * kFew * kOLd * 4);  // [2][4][kFew]
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -561,14 +565,16 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   const int vis0 = row_limit(a, it, 0, kend);              // by the first row
   const int vis1 = min(it.vis_end, kend);                  // and by the last
 
-  char* const vt = smem + wave * kVTile;
-  const int vkg = lane & 7;   // keys 4 vkg .. +3 of the tile
-  const int vdg = lane >> 3;  // 16 bytes vdg of a row (bf16: and vdg + 8)
-  u32x4_t kf[kN], vr[kN];
-  int64_t at0, at1;        // pages of the tile's two halves
-  bool ok0 = true, ok1 = true;  // (of the tile in flight)
-  int tile_n = 0;          // in the page numbers at hand
-  // keys past the sequence's end read its last one (their scores are replaced)
+  char* const vt = smem + wave * (kF8 ? kVTile : 2 * kVTile);  // bf16: K tile, then V tile
+  typedef __attribute__((address_space(3))) char lds_char;
+  lds_char* ring = (lds_char*)vt;
+  asm volatile("" : "+s"(ring));  // (see paged_tile)
+  const int vkg = lane & 7;   // 8-bit: keys 4 vkg .. +3 of the tile
+  const int vdg = lane >> 3;  // values 16 vdg .. +15 of a row
+  u32x4_t kf[kF8 ? 4 : 8], vr[kF8 ? 4 : 8];
+  int64_t at0, at1;             // pages of the two halves of the tile to fetch
+  bool ok0 = true, ok1 = true;  // (8-bit: of the tile in flight)
+  int tile_n = 0;               // in the page numbers at hand
   auto next_pages = [&](int k0) __attribute__((always_inline)) {
     if (tile_n == 32) {
       load_pages(k0);
@@ -582,21 +588,61 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     ok1 = true;
     if (k0 + 16 < it.nk) at1 = page_at<kF8>(a, kvh, p1, ok1);
   };
+  // bf16: 16 keys of one page by four DMAs; rows behind the sequence's end, and
+  // all of a page that is none, come as zeros
+  const int kr_sub = lane >> 4, kpc = lane & 15;
+  uint32_t kvo[4], vvo = 0, koff = 0, voff[4];
+  if constexpr (!kF8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) kvo[i] = (uint32_t)((4 * i + kr_sub) * kRowB + ((kpc ^ (4 * i + kr_sub)) << 4));
+    vvo = (uint32_t)(kr_sub * kRowB + ((kpc ^ (kr_sub << 2)) << 4));
+    koff = (uint32_t)(lrow * kRowB + ((lhalf ^ (lrow & 15)) << 4));  // K chunk 2 s + lhalf: ^ (s << 5)
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      const int key = (lane >> 2) & 3;
+      const int c = ((db ^ key) << 2) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      voff[db] = (uint32_t)(kVTile + (4 * lhalf + key) * kRowB + (c << 4) + 8 * (lane & 1));
+    }
+  }
+  auto half_rsrc = [&](const char* pool, int k0, int h) __attribute__((always_inline)) {
+    const int key = k0 + 16 * h;
+    const int n = (h ? ok1 : ok0) ? clampi(it.nk - key, 0, 16) : 0;
+    return make_rsrc(pool + (h ? at1 : at0) + (uint32_t)(key & mask) * kRowB, (uint32_t)(n * kRowB));
+  };
+  // 8-bit: keys past the sequence's end read its last one (their scores are replaced)
   auto row_at = [&](int k0, int kk) __attribute__((always_inline)) {
     const int key = min(k0 + kk, it.nk - 1);
     return (key - k0 >= 16 ? at1 : at0) + (int64_t)(key & mask) * kPageRow<kF8>;
   };
   auto load_k = [&](int k0) __attribute__((always_inline)) {
-    const char* p = a.k + row_at(k0, lrow) + lhalf * 16;
+    if constexpr (kF8) {
+      const char* p = a.k + row_at(k0, lrow) + lhalf * 16;
 #pragma unroll
-    for (int s = 0; s < kN; ++s) kf[s] = *reinterpret_cast<const u32x4_t*>(p + s * 32);
+      for (int s = 0; s < 4; ++s) kf[s] = *reinterpret_cast<const u32x4_t*>(p + s * 32);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const __amdgpu_buffer_rsrc_t rs = half_rsrc(a.k, k0, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, ring + (16 * h + 4 * i) * kRowB, 16, (int)kvo[i], 0, 0, 0);
+      }
+    }
   };
   auto load_v = [&](int k0) __attribute__((always_inline)) {
+    if constexpr (kF8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const char* p = a.v + row_at(k0, 4 * vkg + i) + vdg * 16;
-      vr[i] = *reinterpret_cast<const u32x4_t*>(p);
-      if constexpr (!kF8) vr[4 + i] = *reinterpret_cast<const u32x4_t*>(p + 128);
+      for (int i = 0; i < 4; ++i)
+        vr[i] = *reinterpret_cast<const u32x4_t*>(a.v + row_at(k0, 4 * vkg + i) + vdg * 16);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const __amdgpu_buffer_rsrc_t rs = half_rsrc(a.v, k0, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, ring + kVTile + (16 * h + 4 * i) * kRowB, 16, (int)vvo,
+                                                   4 * i * kRowB, 0, 0);
+      }
     }
   };
 
@@ -614,11 +660,11 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   }
   for (; k0 < vis1; k0 += step) {
     const bool more = k0 + step < vis1;
-    if (!(ok0 && ok1)) {  // a page that is none reads as zeros
+    if (kF8 && !(ok0 && ok1)) {  // a page that is none reads as zeros
       const bool kz = (lrow >= 16 && k0 + 16 < it.nk) ? !ok1 : !ok0;
       const bool vz = (vkg >= 4 && k0 + 16 < it.nk) ? !ok1 : !ok0;
 #pragma unroll
-      for (int s = 0; s < kN; ++s) {
+      for (int s = 0; s < 4; ++s) {
         if (kz) kf[s] = u32x4_t{0, 0, 0, 0};
         if (vz) vr[s] = u32x4_t{0, 0, 0, 0};
       }
@@ -633,16 +679,25 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
         mfma_step<true>(sc, u32x4_t{x0.x, x0.y, x1.x, x1.y}, qf[2 * s]);
         mfma_step<true>(s2, u32x4_t{x2.x, x2.y, x3.x, x3.y}, qf[2 * s + 1]);
       }
+      if (more) {
+        next_pages(k0 + step);
+        load_k(k0 + step);
+      }
     } else {
+      wait_vmcnt<8>();  // K is there, V still comes
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int s = 0; s < 8; ++s) kf[s] = lds_read16(vt, (int)(koff ^ (s << 5)));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next tile takes its place
+      if (more) {
+        next_pages(k0 + step);
+        load_k(k0 + step);
+      }
 #pragma unroll
       for (int s = 0; s < 8; s += 2) {
         mfma_step<true>(sc, kf[s], qf[s]);
         mfma_step<true>(s2, kf[s + 1], qf[s + 1]);
       }
-    }
-    if (more) {
-      next_pages(k0 + step);
-      load_k(k0 + step);
     }
     sc += s2;
     if (k0 + kBK > vis0) {
@@ -676,42 +731,50 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     for (int st = 0; st < 2; ++st)
 #pragma unroll
       for (int i = 0; i < 4; ++i) pf[st][i] = pack_bf16(sc[8 * st + 2 * i], sc[8 * st + 2 * i + 1]);
-    // V tile to LDS, transposed (a wave's own tile: its LDS operations are in
-    // order, so no barrier)
-    auto put = [&](int d, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3, bool odd) __attribute__((always_inline)) {
-      const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
-      *reinterpret_cast<u32x2_t*>(vt + vt_off(d, (uint32_t)vkg)) =
-          u32x2_t{__builtin_amdgcn_perm(v1, v0, sel), __builtin_amdgcn_perm(v3, v2, sel)};
-    };
+    // O^T += V^T P^T over 2 steps of 16 keys, in the scores' key order
     if constexpr (kF8) {
+      // V tile to LDS, transposed (a wave's own tile: its LDS operations are in
+      // order, so no barrier)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         u32x2_t y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = e4m3_to_bf16(vr[i][w]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          put(16 * vdg + 4 * w + e, y[0][e >> 1], y[1][e >> 1], y[2][e >> 1], y[3][e >> 1], e & 1);
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+          *reinterpret_cast<u32x2_t*>(vt + vt_off(16 * vdg + 4 * w + e, (uint32_t)vkg)) =
+              u32x2_t{__builtin_amdgcn_perm(y[1][e >> 1], y[0][e >> 1], sel),
+                      __builtin_amdgcn_perm(y[3][e >> 1], y[2][e >> 1], sel)};
+        }
       }
+      if (more) load_v(k0 + step);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+          const u32x2_t lo = *reinterpret_cast<const u32x2_t*>(vt + vt_off(32 * db + lrow, (uint32_t)(4 * st + lhalf)));
+          const u32x2_t hi =
+              *reinterpret_cast<const u32x2_t*>(vt + vt_off(32 * db + lrow, (uint32_t)(4 * st + lhalf + 2)));
+          mfma_step<true>(oacc[db], u32x4_t{lo.x, lo.y, hi.x, hi.y}, pf[st]);
+        }
     } else {
+      if (more)
+        wait_vmcnt<8>();  // V is there, the next K still comes
+      else
+        wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          put(64 * c + 8 * vdg + e, vr[4 * c][e >> 1], vr[4 * c + 1][e >> 1], vr[4 * c + 2][e >> 1],
-              vr[4 * c + 3][e >> 1], e & 1);
-    }
-    if (more) load_v(k0 + step);
-    // O^T += V^T P^T over 2 steps of 16 keys, in the scores' key order
-#pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-      for (int db = 0; db < 4; ++db) {
-        const u32x2_t lo = *reinterpret_cast<const u32x2_t*>(vt + vt_off(32 * db + lrow, (uint32_t)(4 * st + lhalf)));
-        const u32x2_t hi =
-            *reinterpret_cast<const u32x2_t*>(vt + vt_off(32 * db + lrow, (uint32_t)(4 * st + lhalf + 2)));
-        mfma_step<true>(oacc[db], u32x4_t{lo.x, lo.y, hi.x, hi.y}, pf[st]);
+      for (int i = 0; i < 8; ++i) {
+        const char* const p = vt + voff[i & 3] + 16 * (i >> 2) * kRowB;
+        const u32x2_t lo = lds_read_tr(p), hi = lds_read_tr(p + 8 * kRowB);
+        vr[i] = u32x4_t{lo.x, lo.y, hi.x, hi.y};
       }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) load_v(k0 + step);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mfma_step<true>(oacc[i & 3], vr[i], pf[i >> 2]);
+    }
   }
   if (vis0 < vis1 && any_nan(oacc))
     paged_redo<kF8, kF8>(a, it.b, kvh, qf, oacc, m_run, c2, vis, kbeg + wave * kBK, step, vis1);

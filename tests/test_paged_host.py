@@ -118,8 +118,8 @@ def test_workspace():
     assert 0 < need <= 35 << 20
     assert attend(c, a, ws=None) == attend(c, a, ws_bytes=need - 1) == attend(c, a, ws=FAKE + 16) == WS
     # short sequences are never cut; more than 256 are planned in memory; no rows need nothing
-    assert size(cache(max_pages=31), a) == 0
-    assert 0 < size(cache(max_pages=31, B=300), a) <= 4096
+    assert size(cache(max_pages=15), a) == 0
+    assert 0 < size(cache(max_pages=15, B=300), a) <= 8192
     assert size(c, attn(q_capacity=0)) == 0
     for B in (1, 256, 257, 65535):
         for hkv in (1, 2, 4, 60):
