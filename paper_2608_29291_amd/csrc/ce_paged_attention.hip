@@ -261,8 +261,10 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
 hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
   if (a.q_cap <= 0) return hipSuccess;
   const PagedGrid p = paged_grid(a.B, a.H, a.Hkv, a.q_cap, (int64_t)a.max_pages << a.page_log2);
-  // Items of one tile a sequence share no keys; others in groups of neighbours.
-  const int group = (int64_t)a.q_cap * (a.H / a.Hkv) <= (int64_t)kFew * a.B ? 1 : 16;
+  // Items of one tile a sequence share no keys; others in groups of neighbours
+  // (groups of 1, 4, 16, 32: 512 queries over 8704 keys 75.5, 76.2, 79.2, 79.9 us, four
+  // chunks of 2048 over 7000 to 10240 888, 883, 896, 881).
+  const int group = (int64_t)a.q_cap * (a.H / a.Hkv) <= (int64_t)kFew * a.B ? 1 : 4;
   const int64_t unit = (int64_t)kXcdCount * group;
   const int64_t grid = (p.items + unit - 1) / unit * unit;
   a.grid = (uint32_t)grid;

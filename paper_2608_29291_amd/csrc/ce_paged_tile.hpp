@@ -324,9 +324,10 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item&
     it.slot = (int)(f.slots + u * C);
     u += f.whole;
   } else if (C > 1 && u >= f.whole) {
-    const uint32_t v = u - f.whole;
-    const uint32_t back = v / (uint32_t)C;
-    it.c = (int)(v - back * C);
+    // all units' first chunks, then their second: neighbours read the same keys
+    const uint32_t v = u - f.whole, n = (uint32_t)f.size.tiles * a.Hkv - f.whole;
+    it.c = (int)(v / n);
+    const uint32_t back = v - it.c * n;
     it.slot = (int)(f.slots + back * C);
     u = f.whole + back;
   } else {
@@ -339,6 +340,9 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item&
   it.rows = min(kPagedRows, it.nq * g - r0);
   it.vis_end = row_limit(a, it, (r0 + it.rows - 1) / g, it.nk);
   it.n_chunks = C > 1 ? max(1, (int)(((uint32_t)it.vis_end + it.chunk - 1) / (uint32_t)it.chunk)) : 1;
+  // (all of it is the wave's, but the divisions leave it in vector registers)
+  for (int* const p : {&it.kvh, &it.tile, &it.chunk, &it.c, &it.n_chunks, &it.slot, &it.rows, &it.vis_end})
+    *p = __builtin_amdgcn_readfirstlane(*p);
   return it.c < it.n_chunks;
 }
 
@@ -442,8 +446,9 @@ __device__ __forceinline__ int64_t page_at(const PagedArgs& a, int kvh, int page
 
 // Output of a wave's 32 rows again, key by key (the scores' maximum m and sum are
 // right as they are): keys k0 + n kstep + 0 .. 31 below vis1, a lane's row sees those
-// below vis. qf: the row, chunk s of 8 dims from kDims(s). Slow, and reached only
-// where a value is NaN or infinite in a sequence's last rows.
+// below vis. qf: the row, 8 dims a chunk, chunk s from dim 8 (2 s + lane / 32), or with
+// kWide from 16 (2 (s / 2) + lane / 32) + 8 (s % 2). Slow, and reached only where a
+// value is NaN or infinite in a sequence's last rows.
 template <bool kF8, bool kWide>
 __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, const u32x4_t (&qf)[8], f32x16_t (&oacc)[4],
                                         float m, float c2, int vis, int k0, int kstep, int vis1) {
@@ -459,36 +464,44 @@ __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, c
       const int page = __builtin_amdgcn_readfirstlane(a.table[(int64_t)b * a.max_pages + (j >> a.page_log2)]);
       const int64_t at = page_at<kF8>(a, kvh, page, ok) + (int64_t)(j & mask) * kPageRow<kF8>;
       if (!ok) continue;  // zeros
-      auto value = [&](const char* base, int d) __attribute__((always_inline)) {  // value at dim d of the row
-        if constexpr (kF8) {
-          const uint32_t x = *reinterpret_cast<const uint32_t*>(base + at + (d & ~3));
-          const u32x2_t y = e4m3_to_bf16(x);
-          const uint32_t z = (d & 2) ? y.y : y.x;
-          return bf16_to_f32((d & 1) ? z >> 16 : z & 0xffffu);
-        } else {
-          const uint32_t x = *reinterpret_cast<const uint32_t*>(base + at + 2 * (d & ~1));
-          return bf16_to_f32((d & 1) ? x >> 16 : x & 0xffffu);
-        }
-      };
+      const char* const kp = a.k + at + lhalf * (kF8 && !kWide ? 8 : 16);
+      const char* const vp = a.v + at + lhalf * (kF8 ? 4 : 8);
+      auto lo = [](uint32_t x) __attribute__((always_inline)) { return __uint_as_float(x << 16); };
+      auto hi = [](uint32_t x) __attribute__((always_inline)) { return __uint_as_float(x & 0xffff0000u); };
       float sc = 0.0f;
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const int d0 = kWide ? (2 * (s >> 1) + lhalf) * 16 + 8 * (s & 1) : (2 * s + lhalf) * 8;
+        u32x4_t x;  // the 8 values that meet chunk s of the row
+        if constexpr (kF8) {
+          const u32x2_t y =
+              *reinterpret_cast<const u32x2_t*>(kp + (kWide ? (s >> 1) * 32 + (s & 1) * 8 : s * 16));
+          const u32x2_t e = e4m3_to_bf16(y.x), f = e4m3_to_bf16(y.y);
+          x = u32x4_t{e.x, e.y, f.x, f.y};
+        } else {
+          x = *reinterpret_cast<const u32x4_t*>(kp + s * 32);
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          sc = fmaf(bf16_to_f32((e & 1) ? qf[s][e >> 1] >> 16 : qf[s][e >> 1] & 0xffffu), value(a.k, d0 + e), sc);
+        for (int e = 0; e < 4; ++e) sc = fmaf(hi(qf[s][e]), hi(x[e]), fmaf(lo(qf[s][e]), lo(x[e]), sc));
         __builtin_amdgcn_sched_barrier(0);  // (few registers are left)
       }
       sc += __shfl_xor(sc, 32);
       const float p = __builtin_amdgcn_exp2f(fmaf(sc, c2, -mc));
       if (j < vis) {
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            oacc[db][v] = fmaf(p, value(a.v, 32 * db + 8 * (v >> 2) + 4 * lhalf + (v & 3)), oacc[db][v]);
-            if ((v & 3) == 3) __builtin_amdgcn_sched_barrier(0);
-          }
+        for (int v = 0; v < 16; ++v) {  // dims 8 v + 4 lhalf .. +3
+          u32x2_t x;
+          if constexpr (kF8)
+            x = e4m3_to_bf16(*reinterpret_cast<const uint32_t*>(vp + v * 8));
+          else
+            x = *reinterpret_cast<const u32x2_t*>(vp + v * 16);
+          f32x16_t& o = oacc[v >> 2];
+          const int r = 4 * (v & 3);
+          o[r] = fmaf(p, lo(x.x), o[r]);
+          o[r + 1] = fmaf(p, hi(x.x), o[r + 1]);
+          o[r + 2] = fmaf(p, lo(x.y), o[r + 2]);
+          o[r + 3] = fmaf(p, hi(x.y), o[r + 3]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
 }
@@ -500,6 +513,13 @@ __device__ __forceinline__ bool any_nan(const f32x16_t (&oacc)[4]) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) t = fmaf(oacc[i][v], 0.0f, t);  // (infinities too: no harm)
   return __builtin_amdgcn_ballot_w64(t != t) != 0;
+}
+
+// Buffer over a wave's rows. A size that a vector instruction gave (a clamp has no
+// scalar one) would make every load through it a loop over the lanes' buffers
+// (4 x 2176 queries over 2304 keys: 148 us with such loops, 140 without).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t wave_rsrc(const void* base, uint32_t bytes) {
+  return make_rsrc(base, (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes));
 }
 
 // ------------------------------------------------------------------ few rows
@@ -607,7 +627,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   auto half_rsrc = [&](const char* pool, int k0, int h) __attribute__((always_inline)) {
     const int key = k0 + 16 * h;
     const int n = (h ? ok1 : ok0) ? clampi(it.nk - key, 0, 16) : 0;
-    return make_rsrc(pool + (h ? at1 : at0) + (uint32_t)(key & mask) * kRowB, (uint32_t)(n * kRowB));
+    return wave_rsrc(pool + (h ? at1 : at0) + (uint32_t)(key & mask) * kRowB, (uint32_t)(n * kRowB));
   };
   // 8-bit: keys past the sequence's end read its last one (their scores are replaced)
   auto row_at = [&](int k0, int kk) __attribute__((always_inline)) {
@@ -973,7 +993,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   const uint32_t vvo = opaque((uint32_t)(kr_sub * kRowB + ((kpc ^ (kr_sub << 2)) << 4)));
   u32x4_t kreg[2], vreg[2];  // 8-bit pages: rows 8 i + lane / 8, 16 values lane % 8
   auto fetch_k = [&](const Rows& x, int buf) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.k + x.at, x.bytes);
+    const __amdgpu_buffer_rsrc_t rs = wave_rsrc(a.k + x.at, x.bytes);
     if constexpr (kF8) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) kreg[i] = bload16(rs, lane * 16 + i * 1024, 0);
@@ -985,7 +1005,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     }
   };
   auto fetch_v = [&](const Rows& x, int buf) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.v + x.at, x.bytes);
+    const __amdgpu_buffer_rsrc_t rs = wave_rsrc(a.v + x.at, x.bytes);
     if constexpr (kF8) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) vreg[i] = bload16(rs, lane * 16 + i * 1024, 0);
@@ -1033,8 +1053,10 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   const int vis = row_limit(a, it, qi, kend);  // keys [0, vis) are seen
   const int vis0 = row_limit(a, it, __builtin_amdgcn_readfirstlane(qi), kend);  // by the wave's first row
 
-  using Half0 = std::integral_constant<int, 0>;
-  using Half1 = std::integral_constant<int, 1>;
+  using B0 = std::integral_constant<int, 0>;
+  using B1 = std::integral_constant<int, 1>;
+  using B2 = std::integral_constant<int, 2>;
+  using B3 = std::integral_constant<int, 3>;
   using Yes = std::true_type;
   using No = std::false_type;
   auto tile_max = [&](const f32x16_t& sc) __attribute__((always_inline)) {
@@ -1055,27 +1077,28 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   };
   // operand of MFMA j of a stage: 0..7 the scores (32-byte K step j), 8..15
   // the output (16 keys (j - 8) / 4, 32 dims j % 4)
-  auto frag = [&](int j, int khalf, int vhalf) __attribute__((always_inline)) {
-    if (j < 8) return lds_read16(smem + koff[j], khalf * kBK * kRowB);
-    const char* p = smem + voff[j & 3] + (vhalf * kBK + 16 * ((j - 8) >> 2)) * kRowB;
+  // kb and vb: 32-key blocks of the two K and of the two V buffers
+  auto frag = [&](int j, int kb, int vb) __attribute__((always_inline)) {
+    if (j < 8) return lds_read16(smem + koff[j], kb * kBK * kRowB);
+    const char* p = smem + voff[j & 3] + (vb * kBK + 16 * ((j - 8) >> 2)) * kRowB;
     const u32x2_t lo = lds_read_tr(p), hi = lds_read_tr(p + 8 * kRowB);
     return u32x4_t{lo.x, lo.y, hi.x, hi.y};
   };
-  // One stage takes block blk (32 keys, half blk % 2 of its tile) through the
+  // One stage takes block blk (32 keys) through the
   // softmax (scores sc, lane maximum mt; probabilities to pn) while the matrix
   // cores compute the scores of block blk + 1 (into sn, lane maximum to mn) and
   // then the output of block blk - 1 (probabilities pp): one probability after
   // each MFMA, in program order. The fences keep the compiler from sorting the
   // two kinds of instructions apart again.
-  auto stage = [&](auto half_c, auto first_c, auto last_c, int blk, f32x16_t& sc, f32x16_t& sn, u32x4_t (&pp)[2],
+  auto stage = [&](auto kb_c, auto vb_c, auto first_c, auto last_c, int blk, f32x16_t& sc, f32x16_t& sn, u32x4_t (&pp)[2],
                    u32x4_t (&pn)[2], float mt, float& mn) __attribute__((always_inline)) {
-    constexpr int kHalf = decltype(half_c)::value;
+    constexpr int kKb = decltype(kb_c)::value, kVb = decltype(vb_c)::value;
     constexpr bool kFirst = decltype(first_c)::value, kLast = decltype(last_c)::value;
     constexpr int kLo = kLast ? 8 : 0, kHi = kFirst ? 8 : 16;  // MFMAs of this stage
     constexpr int kPer = 16 / (kHi - kLo);                     // probabilities after each
     u32x4_t fr[16];
 #pragma unroll
-    for (int j = kLo; j < kLo + kAhead; ++j) fr[j] = frag(j, kHalf ^ 1, kHalf ^ 1);
+    for (int j = kLo; j < kLo + kAhead; ++j) fr[j] = frag(j, kKb, kVb);
     // The running maximum moves (and the output is rescaled) only when some
     // lane's block maximum exceeds it by more than kLazy in the exponent, so
     // probabilities stay below 2^kLazy; the sum l uses the same maximum, so
@@ -1113,7 +1136,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = kLo; j < kHi; ++j) {
-      if (j + kAhead < kHi) fr[j + kAhead] = frag(j + kAhead, kHalf ^ 1, kHalf ^ 1);
+      if (j + kAhead < kHi) fr[j + kAhead] = frag(j + kAhead, kKb, kVb);
       if (j == 0) sn = f32x16_t{};
       if (j < 8)
         mfma_step<true>(sn, fr[j], qf[j]);
@@ -1160,7 +1183,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
       const char* qp = a.q + (int64_t)(it.qbase + q0) * a.q_ld + (int64_t)kvh * g * kRowB;
       const int span = h0 + it.rows - last * g;  // heads of that query that are rows
       const __amdgpu_buffer_rsrc_t qrs =
-          make_rsrc(qp, (uint32_t)((int64_t)last * a.q_ld) + (uint32_t)(span * kRowB));
+          wave_rsrc(qp, (uint32_t)((int64_t)last * a.q_ld) + (uint32_t)(span * kRowB));
       const int qb = 2 * kKBytes + 16 * wave * kRowB;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -1208,36 +1231,44 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     for (int j = 0; j < 8; ++j) mfma_step<true>(sa, frag(j, 0, 0), qf[j]);
     ma = tile_max(sa);
     mask(0, sa, ma);
-    stage(Half0{}, Yes{}, No{}, 0, sa, sb, pb, pa, ma, mb);
+    stage(B1{}, B0{}, Yes{}, No{}, 0, sa, sb, pb, pa, ma, mb);
     if constexpr (!kF8) wait_vmcnt<0>();
     __syncthreads();  // every wave has read K of tile 0; V of tile 0 is there
-    for (int t = 0; t + 1 < ntiles; ++t) {
+    // (two tiles a turn: the buffers are immediate offsets)
+    auto turn = [&](int t, auto k0_c, auto k1_c, auto v0_c, auto v1_c) __attribute__((always_inline)) {
+      constexpr int kOdd = decltype(v0_c)::value >> 1;  // t % 2
       const Rows ahead = rows_of(kF8 ? t + 3 : t + 2);
       if constexpr (kF8) {
-        if (t + 2 < ntiles) put(kreg, (t & 1) * kKBytes, true);
-        put(vreg, (2 + ((t + 1) & 1)) * kKBytes, false);
+        if (t + 2 < ntiles) put(kreg, kOdd * kKBytes, true);
+        put(vreg, (2 + (kOdd ^ 1)) * kKBytes, false);
         if (t + 3 < ntiles) fetch_k(ahead, 0);
         if (t + 2 < ntiles) fetch_v(rows1, 0);
       } else {
-        if (t + 2 < ntiles) fetch_k(ahead, t & 1);
+        if (t + 2 < ntiles) fetch_k(ahead, kOdd);
       }
-#pragma unroll
-      for (int s2 = 0; s2 < 8; ++s2) koff[s2] ^= kKBytes;
-      stage(Half1{}, No{}, No{}, 2 * t + 1, sb, sa, pa, pb, mb, ma);
-      if constexpr (!kF8) fetch_v(rows1, (t + 1) & 1);
+      stage(k0_c, v0_c, No{}, No{}, 2 * t + 1, sb, sa, pa, pb, mb, ma);
+      if constexpr (!kF8) fetch_v(rows1, kOdd ^ 1);
       rows1 = ahead;
-      stage(Half0{}, No{}, No{}, 2 * t + 2, sa, sb, pb, pa, ma, mb);
-#pragma unroll
-      for (int db = 0; db < 4; ++db) voff[db] ^= kKBytes;
-      if (t + 4 - tb >= 64) load_pages(t + 1);  // (the next iteration looks three tiles on)
+      stage(k1_c, v1_c, No{}, No{}, 2 * t + 2, sa, sb, pb, pa, ma, mb);
+      if (t + 4 - tb >= 64) load_pages(t + 1);  // (the next turn looks three tiles on)
       if constexpr (!kF8) {
         wait_vmcnt<0>();
         __syncthreads();
       } else {
         lds_barrier();  // (the next tiles' loads stay in flight)
       }
+    };
+    int t = 0;
+    for (; t + 2 < ntiles; t += 2) {
+      turn(t, B2{}, B3{}, B0{}, B1{});
+      turn(t + 1, B0{}, B1{}, B2{}, B3{});
     }
-    stage(Half1{}, No{}, Yes{}, 2 * ntiles - 1, sb, sa, pa, pb, mb, ma);
+    if (t + 1 < ntiles) turn(t, B2{}, B3{}, B0{}, B1{});
+    if ((ntiles & 1) == 0) {
+#pragma unroll
+      for (int db = 0; db < 4; ++db) voff[db] += kKBytes;  // V of the last tile
+    }
+    stage(B0{}, B0{}, No{}, Yes{}, 2 * ntiles - 1, sb, sa, pa, pb, mb, ma);
 #pragma unroll
     for (int j = 8; j < 16; ++j) mfma_step<true>(oacc[j & 3], frag(j, 0, 1), pb[(j - 8) >> 2]);
     const int last_key = min(kend, kbeg + ntiles * kKT);
