@@ -43,7 +43,8 @@ enum {
  *                [n_kv_heads x page_size x head_dim]: the rows of one head are
  *                contiguous, as attention reads them
  *   page_stride  elements between pages, >= n_kv_heads * page_size * head_dim, a
- *                multiple of 16 (several layers may interleave in one allocation)
+ *                multiple of 16, below 2^31 (several layers may interleave in one
+ *                allocation)
  *   k_scale, v_scale  CE_E4M3: device float32 [n_kv_heads], positive and finite, or
  *                both NULL (1): a stored value x stands for x * scale. CE_BF16: NULL
  *   page_table   device int32 [B x max_pages]; entries behind a sequence's last

@@ -28,9 +28,9 @@ struct AppendArgs {
   const char *k_new, *v_new;
   int64_t k_ld, v_ld;  // bytes between rows
   const int32_t* slots;
-  int rows, Hkv, n_slots, page_log2;
+  int rows, Hkv, n_slots, page_log2, rows_per_block;
   char *k, *v;
-  int64_t page_bytes;  // between pages
+  uint32_t page_bytes;  // between pages
   const float *k_scale, *v_scale;
 };
 
@@ -47,7 +47,7 @@ struct PagedArgs {
   const float *ks, *vs;  // scales of 8-bit pages, or NULL
   const int32_t *table, *qo, *lens;
   int64_t q_ld;        // bytes between rows of q
-  int64_t page_bytes;  // bytes between pages
+  uint32_t page_bytes;  // bytes between pages
   int B, H, Hkv, q_cap, n_pages, max_pages, page_log2, causal;
   float scale_log2;  // scale * log2(e)
   int meet_in_launch;  // the chunks of a unit meet in the launch itself
@@ -75,7 +75,7 @@ struct PagedGrid {
 PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys);
 
 hipError_t launch_kv_reserve(ReserveArgs a, hipStream_t stream);
-hipError_t launch_kv_append(const AppendArgs& a, bool e4m3, hipStream_t stream);
+hipError_t launch_kv_append(AppendArgs a, bool e4m3, hipStream_t stream);
 hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream);
 
 }  // namespace ce

@@ -36,7 +36,7 @@ int check_pages(const ce_kv_cache* c) {
   if (c->head_dim != 128 || (c->dtype != CE_BF16 && c->dtype != CE_E4M3)) return CE_ERR_UNSUPPORTED;
   const int64_t page = (int64_t)c->n_kv_heads * c->page_size * 128;
   if (c->page_stride < page || c->page_stride % 16 != 0) return CE_ERR_INVALID_ARG;
-  if (c->page_stride >= (int64_t)1 << 40 || c->n_kv_heads >= 1 << 16) return CE_ERR_UNSUPPORTED;
+  if (c->page_stride >= (int64_t)1 << 31 || c->n_kv_heads >= 1 << 16) return CE_ERR_UNSUPPORTED;
   if (!c->k_scale != !c->v_scale || (c->dtype == CE_BF16 && c->k_scale)) return CE_ERR_INVALID_ARG;
   return CE_OK;
 }
@@ -112,7 +112,7 @@ int ce_kv_append(const ce_kv_cache* cache, const void* k_new, int64_t k_ld, cons
   a.page_log2 = log2_of_page(cache->page_size);
   a.k = static_cast<char*>(cache->k);
   a.v = static_cast<char*>(cache->v);
-  a.page_bytes = cache->page_stride * elem;
+  a.page_bytes = (uint32_t)(cache->page_stride * elem);
   a.k_scale = cache->k_scale;
   a.v_scale = cache->v_scale;
   return hip_status(launch_kv_append(a, cache->dtype == CE_E4M3, static_cast<hipStream_t>(stream)));
@@ -147,7 +147,7 @@ int ce_paged_attention(const ce_kv_cache* cache, const ce_paged_attn* attn, cons
   a.qo = attn->q_offsets;
   a.lens = attn->lens;
   a.q_ld = q_ld * 2;
-  a.page_bytes = cache->page_stride * elem;
+  a.page_bytes = (uint32_t)(cache->page_stride * elem);
   a.B = cache->B;
   a.H = attn->n_heads;
   a.Hkv = cache->n_kv_heads;

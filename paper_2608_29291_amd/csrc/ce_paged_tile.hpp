@@ -441,7 +441,7 @@ constexpr int kPageRow = kF8 ? kDh : kRowB;  // bytes of a row of a page
 template <bool kF8>
 __device__ __forceinline__ int64_t page_at(const PagedArgs& a, int kvh, int page, bool& ok) {
   ok = (uint32_t)page < (uint32_t)a.n_pages;
-  return (int64_t)(ok ? page : 0) * a.page_bytes + ((int64_t)kvh << a.page_log2) * kPageRow<kF8>;
+  return (int64_t)((uint64_t)(uint32_t)(ok ? page : 0) * a.page_bytes) + ((uint32_t)kvh << a.page_log2) * kPageRow<kF8>;
 }
 
 // Output of a wave's 32 rows again, key by key (the scores' maximum m and sum are
