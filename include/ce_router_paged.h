@@ -138,7 +138,7 @@ typedef struct ce_paged_attn {
 
 /*
  *   q   device bf16: row r at r * q_ld elements, its n_heads x head_dim values
- *       contiguous; q_ld a multiple of 8, below 2^23
+ *       contiguous; q_ld a multiple of 8, below 2^22
  *   o   device bf16 [q_capacity x n_heads x head_dim] out (rows of real queries only)
  *   ws  device workspace of ce_paged_workspace_size(cache, attn) bytes, 256-byte
  *       aligned, contents on entry do not matter. Calls that may overlap, captured
@@ -148,7 +148,8 @@ typedef struct ce_paged_attn {
  * probabilities are rounded to bf16 for the product with V. Deterministic.
  * Errors: CE_ERR_INVALID_ARG for null pointers, sizes, a scale that is not a
  * positive finite number or causal outside {0, 1}; CE_ERR_UNSUPPORTED outside
- * the limits or for q_capacity * n_heads >= 2^29 or B * n_kv_heads >= 2^22;
+ * the limits, for more than 4096 query heads a key/value head, q_capacity * n_heads
+ * >= 2^29 or B * n_kv_heads >= 2^22;
  * CE_ERR_WORKSPACE; CE_ERR_HIP.
  * ce_paged_workspace_size depends on the sizes in cache and attn only (no device
  * pointer is read), is at most 35 MB, and 0 where none is used or the call

@@ -50,25 +50,24 @@ struct PagedArgs {
   uint32_t page_bytes;  // bytes between pages
   int B, H, Hkv, q_cap, n_pages, max_pages, page_log2, causal;
   float scale_log2;  // scale * log2(e)
-  int meet_in_launch;  // the chunks of a unit meet in the launch itself
+  int decode;        // a call of single tokens (the plan: ce_paged_tile.hpp)
   uint32_t grid;     // items that the launch has workgroups for
-  float* part;       // partial results, kPagedPart floats a slot
-  unsigned long long* arrived;  // counters of the chunks that meet, kPagedTarget a level
+  float* part;       // partial results, a slot for each place
+  unsigned long long* arrived;  // counters of the chunks that meet, kPagedPlaces a level
   unsigned long long token;     // of this call, 48 bits
   PagedPlan* plan;   // B > kPagedScan: the sequences, then the totals and (whole) the chunk length
 };
 
 constexpr int kPagedScan = 256;    // sequences that a wave plans by itself (four a lane)
-constexpr int kPagedTarget = 512;  // places for workgroups: two on each CU
-constexpr int kPagedRows = 128;    // (query, head) rows of a tile
-constexpr int kPagedPart = kPagedRows * (128 + 2);  // floats of a slot: outputs, maxima, sums
-
+constexpr int kPagedFew = 32;     // (query, head) rows of a tile of single tokens
+constexpr int kPagedTile = 128;   // and of one of many rows
+constexpr int kPagedPlaces = 512; // places for workgroups: two on each CU
 constexpr int kPagedLevels = 3;    // sixteen chunks meet at a time, 512 at most
 
 // What the host knows of a call: the workgroups that any batch of these sizes needs.
 struct PagedGrid {
   int64_t items;
-  int meet_in_launch;
+  int decode;
   int cut_units;  // for the launch that adds chunks up, at most (0: no such launch)
   size_t plan_bytes, count_bytes, bytes;  // workspace: the plan, arrival counters, partial results
 };

@@ -46,6 +46,7 @@ int check_attn(const ce_kv_cache* c, const ce_paged_attn* at) {
   const int s = check_pages(c);
   if (s != CE_OK) return s;
   if (!at || at->n_heads < 1 || at->n_heads % c->n_kv_heads != 0 || at->q_capacity < 0) return CE_ERR_INVALID_ARG;
+  if (at->n_heads / c->n_kv_heads > 4096) return CE_ERR_UNSUPPORTED;
   if (at->causal != 0 && at->causal != 1) return CE_ERR_INVALID_ARG;
   if (!isfinite(at->scale) || !(at->scale > 0.0f)) return CE_ERR_INVALID_ARG;
   if ((int64_t)at->q_capacity * at->n_heads >= (int64_t)1 << 29 || (int64_t)c->B * c->n_kv_heads >= (int64_t)1 << 22)
@@ -127,7 +128,7 @@ int ce_paged_attention(const ce_kv_cache* cache, const ce_paged_attn* attn, cons
   const int s = check_attn(cache, attn);
   if (s != CE_OK) return s;
   if (q_ld < (int64_t)attn->n_heads * 128 || q_ld % 8 != 0) return CE_ERR_INVALID_ARG;
-  if (q_ld >= (int64_t)1 << 23) return CE_ERR_UNSUPPORTED;
+  if (q_ld >= (int64_t)1 << 22) return CE_ERR_UNSUPPORTED;
   if (!attn->q_offsets || !attn->lens) return CE_ERR_INVALID_ARG;
   if (attn->q_capacity > 0 && (!q || !o || !cache->k || !cache->v || !cache->page_table)) return CE_ERR_INVALID_ARG;
   const PagedGrid p = grid_of(cache, attn);

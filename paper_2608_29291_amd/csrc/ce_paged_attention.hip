@@ -39,19 +39,28 @@ namespace {
 
 using namespace paged;
 
+// Workgroup w runs on XCD w % 8: an XCD takes `group` neighbouring items at a time, whose
+// tiles of one sequence and head find each other's keys in its L2.
+__device__ __forceinline__ uint32_t item_of(uint32_t w, uint32_t group) {
+  const uint32_t in_xcd = w / kXcdCount;
+  return in_xcd / group * (kXcdCount * group) + (w % kXcdCount) * group + in_xcd % group;
+}
+
+template <bool kF8>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_decode_kernel(PagedArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[kSmem];
+  Item it;
+  if (find_item<false>(a, blockIdx.x, it)) paged_few<kF8, true>(a, smem, it);
+}
+
 template <bool kF8>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_attention_kernel(PagedArgs a,
-                                                                                                        int group) {
+                                                                                                        uint32_t group) {
   __shared__ __attribute__((aligned(1024))) char smem[kSmem];
-  // Workgroup w runs on XCD w % 8: an XCD takes `group` neighbouring items at a
-  // time, whose tiles of one sequence and head find each other's keys in its L2.
-  const int w = blockIdx.x;
-  const int in_xcd = w / kXcdCount;
-  const uint32_t at = (in_xcd / group) * (kXcdCount * group) + (w % kXcdCount) * group + in_xcd % group;
   Item it;
-  if (!find_item<false>(a, at, it)) return;
+  if (!find_item<false>(a, item_of(blockIdx.x, group), it)) return;
   if (it.few)
-    paged_few<kF8>(a, smem, it);
+    paged_few<kF8, false>(a, smem, it);
   else
     paged_tile<kF8>(a, smem, it);
 }
@@ -96,7 +105,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
   for (int b = tid; b < a.B; b += 512) {
     const Size s = size_of(a, b, g);
     const uint32_t n = (uint32_t)s.tiles * a.Hkv;
-    const float c = n ? cost_of(s, g) : 0.0f;
+    const float c = n ? cost_of(a, s, g) : 0.0f;
     w += (float)n * c;
     units += n;
     most = fmaxf(most, c);
@@ -117,7 +126,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
     const uint32_t n = (uint32_t)s.tiles * a.Hkv;
     const int64_t first = base + scan(n, total);
     const uint32_t wh = whole_of(a, s, (uint32_t)min(first, (int64_t)1 << 30), whole);
-    rest += (float)(n - wh) * cost_of(s, g);
+    rest += (float)(n - wh) * cost_of(a, s, g);
     if (b < a.B) a.plan[b].whole = wh;
     base += total;
   }
@@ -148,7 +157,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
       a.plan[a.B].whole = (uint32_t)L;
     }
     // (as in find_by_scan)
-    if (L == 1 << 30 || (items <= a.grid && slots <= kPagedTarget)) break;
+    if (L == 1 << 30 || (items <= a.grid && slots <= kPagedPlaces)) break;
     L = 1 << 30;
   }
 }
@@ -163,10 +172,11 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
   const int n = it.n_chunks;
   const float c2 = a.scale_log2 * (a.ks ? a.ks[it.kvh] : 1.0f);
   const float vs = a.vs ? a.vs[it.kvh] : 1.0f;
-  const float* const slot = a.part + (int64_t)it.slot * kPagedPart;
+  constexpr int kPart = kSlotBytes<false> / 4;
+  const float* const slot = a.part + (int64_t)it.slot * kPart;
   auto add = [&](auto n_c, auto batch_c, const float* p, int step, int r, auto out) __attribute__((always_inline)) {
     constexpr int kN = decltype(n_c)::value, kBatch = decltype(batch_c)::value;
-    const float* const ps = slot + kPagedRows * kDh + r;
+    const float* const ps = slot + kTileRows * kDh + r;
     float m = -__builtin_inff(), l = 0.0f;
     f32x4_t x[kN];
 #pragma unroll
@@ -176,9 +186,9 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
       f32x4_t y[kBatch][kN];
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const int64_t at = (int64_t)min(c0 + i, n - 1) * kPagedPart;
+        const int64_t at = (int64_t)min(c0 + i, n - 1) * kPart;
         mc[i] = ps[at];
-        lc[i] = ps[at + kPagedRows];
+        lc[i] = ps[at + kTileRows];
 #pragma unroll
         for (int v = 0; v < kN; ++v) y[i][v] = *reinterpret_cast<const f32x4_t*>(p + at + v * step);
       }
@@ -202,7 +212,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
       m = m_new;
     }
     if (r >= it.rows) return;
-    const int row = it.tile * kPagedRows + r;
+    const int row = it.tile * tile_rows(it.few) + r;
     const int qi = row / g;
     const float inv = normalizer(l, vs, row_limit(a, it, qi, it.nk) > 0);
     char* const o = a.o + ((int64_t)(it.qbase + qi) * a.H + it.kvh * g + (row - qi * g)) * kRowB;
@@ -218,7 +228,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
       add(One{}, std::integral_constant<int, 16>{}, slot + at, 0, r, [&](int) { return d; });
     }
   } else {
-    for (int z = blockIdx.y; z < 4 && 32 * z < it.rows; z += gridDim.y)  // accumulators 4 wave .. +3 of wave z
+    for (int z = blockIdx.y; 32 * z < it.rows; z += gridDim.y)  // accumulators 4 wave .. +3
       add(Four{}, Four{}, slot + ((z * 16 + 4 * wave) * 64 + lane) * 4, 256, 32 * z + (lane & 31),
           [&](int v) { return 32 * wave + 8 * v + 4 * (lane >> 5); });
   }
@@ -241,19 +251,22 @@ static uint64_t paged_token() {
 PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
   PagedGrid p = {};
   if (q_cap <= 0) return p;
+  // Single tokens: no more rows than sequences, and no more than eight rows of a
+  // sequence and key/value head for the chunks to meet at once.
+  p.decode = q_cap <= B && H / Hkv <= 8;
   // every sequence with a query adds at most one tile that is not full
-  p.items = ((int64_t)q_cap * (H / Hkv) / kPagedRows + (B < q_cap ? B : q_cap)) * Hkv;
+  const int64_t rows = p.decode ? kPagedFew : kPagedTile;
+  const int64_t units = ((int64_t)q_cap * (H / Hkv) / rows + (B < q_cap ? B : q_cap)) * Hkv;
+  p.items = units;
   if (B > kPagedScan) p.plan_bytes = ((size_t)(B + 1) * sizeof(PagedPlan) + 255) / 256 * 256;
   p.bytes = p.plan_bytes;
   if (max_keys >= 2 * kMinFew) {  // else nothing is cut
-    p.items += kPagedTarget;
-    // Chunks meet in the launch itself where there are no more rows than a thread for
-    // each 16 bytes of a chunk's outputs can take at once: single tokens.
-    p.meet_in_launch = q_cap <= B && H / Hkv <= 8;
-    const int64_t units = ((int64_t)q_cap * (H / Hkv) / kPagedRows + (B < q_cap ? B : q_cap)) * Hkv;
-    if (!p.meet_in_launch) p.cut_units = (int)(units < kPagedTarget / 2 ? units : kPagedTarget / 2);
-    p.count_bytes = (size_t)kPagedLevels * kPagedTarget * sizeof(unsigned long long);
-    p.bytes += p.count_bytes + (size_t)kPagedTarget * kPagedPart * sizeof(float);
+    p.items += kPagedPlaces;
+    if (p.decode)
+      p.count_bytes = (size_t)kPagedLevels * kPagedPlaces * sizeof(unsigned long long);
+    else  // a cut unit has two chunks at least
+      p.cut_units = (int)(units < kPagedPlaces / 2 ? units : kPagedPlaces / 2);
+    p.bytes += p.count_bytes + (size_t)kPagedPlaces * (p.decode ? kSlotBytes<true> : kSlotBytes<false>);
   }
   return p;
 }
@@ -261,27 +274,34 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
 hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
   if (a.q_cap <= 0) return hipSuccess;
   const PagedGrid p = paged_grid(a.B, a.H, a.Hkv, a.q_cap, (int64_t)a.max_pages << a.page_log2);
-  // Items of one tile a sequence share no keys; others in groups of neighbours
-  // (groups of 1, 4, 16, 32: 512 queries over 8704 keys 75.5, 76.2, 79.2, 79.9 us, four
-  // chunks of 2048 over 7000 to 10240 888, 883, 896, 881).
-  const int group = (int64_t)a.q_cap * (a.H / a.Hkv) <= (int64_t)kFew * a.B ? 1 : 4;
-  const int64_t unit = (int64_t)kXcdCount * group;
+  // Groups of 1, 4, 16, 32 neighbours: 512 queries over 8704 keys 75.5, 76.2, 79.2,
+  // 79.9 us, four chunks of 2048 over 7000 to 10240 888, 883, 896, 881.
+  const uint32_t group = 4;
+  const int64_t unit = p.decode ? 1 : (int64_t)kXcdCount * group;
   const int64_t grid = (p.items + unit - 1) / unit * unit;
   a.grid = (uint32_t)grid;
-  a.meet_in_launch = p.meet_in_launch;
+  a.decode = p.decode;
   a.token = paged_token();
   if (a.B > kPagedScan) {
     hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(512), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  const dim3 blocks((unsigned)grid), threads(256);
+  if (p.decode) {
+    if (e4m3)
+      hipLaunchKernelGGL(paged_decode_kernel<true>, blocks, threads, 0, stream, a);
+    else
+      hipLaunchKernelGGL(paged_decode_kernel<false>, blocks, threads, 0, stream, a);
+    return hipGetLastError();
+  }
   if (e4m3)
-    hipLaunchKernelGGL(paged_attention_kernel<true>, dim3((unsigned)grid), dim3(256), 0, stream, a, group);
+    hipLaunchKernelGGL(paged_attention_kernel<true>, blocks, threads, 0, stream, a, group);
   else
-    hipLaunchKernelGGL(paged_attention_kernel<false>, dim3((unsigned)grid), dim3(256), 0, stream, a, group);
+    hipLaunchKernelGGL(paged_attention_kernel<false>, blocks, threads, 0, stream, a, group);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.cut_units == 0) return e;
-  hipLaunchKernelGGL(paged_combine_kernel, dim3(p.cut_units, 4), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(paged_combine_kernel, dim3(p.cut_units, 4), threads, 0, stream, a);
   return hipGetLastError();
 }
 

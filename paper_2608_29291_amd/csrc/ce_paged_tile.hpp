@@ -1,5 +1,5 @@
-// The two workgroups of paged attention (ce_paged_attention.hip): a few rows of a
-// sequence against a chunk of its keys, and a tile of 128 rows.
+// The plan and the two workgroups of paged attention (ce_paged_attention.hip): up to 32
+// rows of a sequence against a chunk of its keys, and a tile of 128 rows.
 #pragma once
 
 #include <type_traits>
@@ -13,11 +13,12 @@ namespace paged {
 
 constexpr int kDh = 128;           // head dimension
 constexpr int kRowB = kDh * 2;     // bytes of a bf16 row
-constexpr int kFew = 32;       // rows of a sequence that paged_few takes
+constexpr int kFew = kPagedFew;
+constexpr int kTileRows = kPagedTile;
 constexpr int kKT = 64;            // keys per tile of paged_tile
 constexpr int kBK = 32;            // keys per block: one pass of the softmax
 constexpr int kKBytes = kKT * kRowB;
-constexpr int kAhead = 3;          // MFMA operands read from LDS this many products ahead
+constexpr int kGroup = 4;          // MFMA operands read from LDS together, one group ahead
 constexpr float kLazy = 8.0f;      // headroom of the running maximum (exponent of 2)
 constexpr int kMinFew = 128;       // least keys of a chunk: one tile of 32 for each wave
 constexpr int kMinTile = 256;
@@ -26,17 +27,21 @@ constexpr int kOLd = kDh + 4;      // floats per row of paged_few's outputs in L
 constexpr int kVRow = kBK * 2;     // bytes per row of paged_few's V^T
 constexpr int kVTile = kDh * kVRow;
 constexpr int kSmem = 4 * kFew * kOLd * 4 + 2 * 4 * kFew * 4;
-static_assert(kSmem >= 4 * kKBytes && kSmem >= 4 * kVTile, "the tiles fit");
+static_assert(kSmem >= 4 * 2 * kVTile && kSmem >= 4 * kKBytes && 2 * kSmem <= 160 * 1024, "the tiles fit");
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
 // ------------------------------------------------------------------ the plan
 //
+// A call of single tokens (a.decode: no more rows than sequences) takes its rows 32 at
+// a time (paged_few); any other takes those of a sequence that has more than 32 in
+// tiles of 128 (paged_tile).
+//
 // A unit is a row tile of a sequence for one key/value head; units are numbered
 // sequence by sequence, head by head, the last tiles first (under a causal mask they
 // see the most keys). A key costs a tile of 128 rows about twice what it costs a few
-// rows, so keys are counted as 1 and 1/2. With S = 512 places for workgroups (two on
-// each CU) and A = (sum of the units' keys) / S:
+// rows, so keys are counted as 1 and 1/2. With S = 512 places for workgroups (two on each
+// CU) and A = (sum of the units' keys) / S:
 //   * a batch of many units fills S places some whole number of times and leaves
 //     a rest; the units before the rest are whole, and the rest, fewer than S, are cut
 //     along their keys so that they too fill the places: L = (their keys) / S;
@@ -46,23 +51,25 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 // are at most S (a second round of a few would double the time) and as many
 // partial results fit the workspace.
 //
-// How the chunks meet: of a few rows, in the launch itself (a second one would cost
-// 5 us of 18); of many rows, by a second launch over the whole chip, since one
-// workgroup would read 64 KB a chunk (a.meet_in_launch, from the host: then only
-// the few-row units are cut).
+// How the chunks meet: of single tokens, in the launch itself (a second one would
+// cost 5 us of 18); of many rows, by a second launch over the whole chip, since one
+// workgroup would read 64 KB a chunk.
 
 struct Size {
   int qbase, nq, nk, tiles;
 };
 
-__device__ __forceinline__ bool is_few(int nq, int g) { return nq * g <= kFew; }
+__device__ __forceinline__ bool is_few(const PagedArgs& a, int nq, int g) { return a.decode || nq * g <= kFew; }
+
+__device__ __forceinline__ int tile_rows(bool few) { return few ? kFew : kTileRows; }
 
 __device__ __forceinline__ Size size_from(const PagedArgs& a, int q0, int q1, int len, int g) {
   Size s;
   s.qbase = clampi(q0, 0, a.q_cap);
   s.nq = clampi(q1, s.qbase, a.q_cap) - s.qbase;
   s.nk = clampi(len, 0, a.max_pages << a.page_log2);
-  s.tiles = (s.nq * g + kPagedRows - 1) / kPagedRows;
+  const int rows = tile_rows(is_few(a, s.nq, g));
+  s.tiles = (s.nq * g + rows - 1) / rows;
   return s;
 }
 
@@ -72,20 +79,19 @@ __device__ __forceinline__ Size size_of(const PagedArgs& a, int b, int g) {
 
 // Units before the rest, of n in all that cost w, the dearest `most`.
 __device__ __forceinline__ uint32_t whole_units(uint32_t n, float w, float most) {
-  return most * (0.5f * kPagedTarget) >= w ? 0 : n / kPagedTarget * kPagedTarget;
+  return most * (0.5f * kPagedPlaces) >= w ? 0 : n / kPagedPlaces * kPagedPlaces;
 }
 
 // Keys per chunk where the units that may be cut have w keys.
 __device__ __forceinline__ int chunk_length(float w) {
-  const float l = w * (1.0f / kPagedTarget);
+  const float l = w * (1.0f / kPagedPlaces);
   return l > 1e9f ? 1 << 30 : (int)l + 1;
 }
 
 // A sequence's chunks (a whole number of its waves' tiles).
 __device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, int& C, int& chunk) {
-  const bool few = is_few(s.nq, g);
+  const bool few = is_few(a, s.nq, g);
   C = s.nk / (few ? max(2 * min(L, 1 << 29), kMinFew) : max(L, kMinTile));
-  if (!few && a.meet_in_launch) C = 1;
   chunk = s.nk;
   if (C > 1) {
     const int unit = few ? kBK : kKT;
@@ -105,8 +111,8 @@ __device__ __forceinline__ uint32_t whole_of(const PagedArgs& a, const Size& s, 
 }
 
 // Its keys as the plan counts them, per unit.
-__device__ __forceinline__ float cost_of(const Size& s, int g) {
-  return (float)s.nk * (is_few(s.nq, g) ? 0.5f : 1.0f);
+__device__ __forceinline__ float cost_of(const PagedArgs& a, const Size& s, int g) {
+  return (float)s.nk * (is_few(a, s.nq, g) ? 0.5f : 1.0f);
 }
 
 // Its items, its partial results and the units that have such.
@@ -200,7 +206,7 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
     s[i] = Size{0, 0, 0, 0};
     if (b < a.B) s[i] = size_of(a, b, g);
     const uint32_t n = (uint32_t)s[i].tiles * a.Hkv;
-    const float c = n ? cost_of(s[i], g) : 0.0f;
+    const float c = n ? cost_of(a, s[i], g) : 0.0f;
     w += (float)n * c;
     units += n;
     most = fmaxf(most, c);
@@ -208,14 +214,14 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
   const uint32_t units_to = wave_scan(units);
   w = wave_sum(w);
   const uint32_t all = __builtin_amdgcn_readlane(units_to, 63);
-  const uint32_t whole = all < (uint32_t)kPagedTarget ? 0 : whole_units(all, w, wave_max(most));
+  const uint32_t whole = whole_units(all, w, wave_max(most));
   if (whole) {  // what the rest costs
     float rest = 0.0f;
     uint32_t first = units_to - units;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const uint32_t n = (uint32_t)s[i].tiles * a.Hkv;
-      rest += (float)(n - whole_of(a, s[i], first, whole)) * cost_of(s[i], g);
+      rest += (float)(n - whole_of(a, s[i], first, whole)) * cost_of(a, s[i], g);
       first += n;
     }
     w = wave_sum(rest);
@@ -243,7 +249,7 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
     // offsets are out of order. Then nothing is cut (every chunk of a cut unit
     // must run) and what lies past the grid is left.
     if (f.L == 1 << 30 ||
-        (items_all <= a.grid && __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedTarget))
+        (items_all <= a.grid && __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedPlaces))
       break;
     f.L = 1 << 30;
   }
@@ -314,7 +320,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item&
   it.qbase = f.size.qbase;
   it.nq = f.size.nq;
   it.nk = f.size.nk;
-  it.few = is_few(it.nq, g);
+  it.few = is_few(a, it.nq, g);
   int C;
   cut(a, f.size, g, f.L, C, it.chunk);
   uint32_t u = at - f.before;
@@ -336,8 +342,8 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item&
   }
   it.kvh = (int)(u / (uint32_t)f.size.tiles);
   it.tile = f.size.tiles - 1 - (int)(u - (uint32_t)it.kvh * f.size.tiles);
-  const int r0 = it.tile * kPagedRows;
-  it.rows = min(kPagedRows, it.nq * g - r0);
+  const int r0 = it.tile * tile_rows(it.few);
+  it.rows = min(tile_rows(it.few), it.nq * g - r0);
   it.vis_end = row_limit(a, it, (r0 + it.rows - 1) / g, it.nk);
   it.n_chunks = C > 1 ? max(1, (int)(((uint32_t)it.vis_end + it.chunk - 1) / (uint32_t)it.chunk)) : 1;
   // (all of it is the wave's, but the divisions leave it in vector registers)
@@ -368,11 +374,17 @@ __device__ __forceinline__ float normalizer(float l, float vs, bool sees) {
 // sums move by device-coherent (sc1) stores and loads, and a workgroup arrives when
 // its stores have completed, so no cache is written back or dropped.
 constexpr int kSC1 = 16;            // cache-policy operand: sc1
-constexpr uint32_t kSlotBytes = kPagedPart * 4;
-constexpr uint32_t kStats = kPagedRows * kDh * 4;  // maxima, then sums, behind a slot's outputs
+// A slot: outputs of its rows, then their maxima, then their sums.
+template <bool kDecode>
+constexpr uint32_t kSlotRows = kDecode ? kFew : kTileRows;
+template <bool kDecode>
+constexpr uint32_t kSlotBytes = kSlotRows<kDecode> * (kDh + 2) * 4;
+template <bool kDecode>
+constexpr uint32_t kStats = kSlotRows<kDecode> * kDh * 4;
 
+template <bool kDecode>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t part_rsrc(const PagedArgs& a) {
-  return make_rsrc(a.part, (uint32_t)kPagedTarget * kSlotBytes);
+  return make_rsrc(a.part, kPagedPlaces * kSlotBytes<kDecode>);
 }
 __device__ __forceinline__ void part_store4(__amdgpu_buffer_rsrc_t rs, uint32_t at, float x, float y, float z, float w) {
   const u32x4_t v = {__float_as_uint(x), __float_as_uint(y), __float_as_uint(z), __float_as_uint(w)};
@@ -430,8 +442,8 @@ __device__ __forceinline__ u32x2_t e4m3_to_bf16(uint32_t x) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true))};
 }
 
-// x / g for 0 <= x < kPagedRows + g: off by at most 2^-22 x / g, while x + 1/2 is at
-// least 1 / (2 g) from a multiple.
+// x / g for 0 <= x < kTileRows + g, g <= 4096: off by at most 2^-22 x / g, while x + 1/2
+// is at least 1 / (2 g) from a multiple.
 __device__ __forceinline__ int small_div(int x, float inv_g) { return (int)(((float)x + 0.5f) * inv_g); }
 
 template <bool kF8>
@@ -542,7 +554,7 @@ __device__ __forceinline__ uint32_t vt_off(int d, uint32_t u) {
 //   * 8-bit: K straight to registers in operand order (a line in four loads as well,
 //     but half the bytes: at the copy rate for long caches), V through
 //     registers, converted, exactly, and stored transposed in LDS.
-template <bool kF8>
+template <bool kF8, bool kDecode>
 __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, const Item& it) {
   float* const ml = reinterpret_cast<float*>(smem + 4 * kFew * kOLd * 4);  // [2][4][kFew]
   const int tid = threadIdx.x;
@@ -569,9 +581,11 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   // ---- the query row of this lane ----
   const int lrow = lane & 31;
   const int lhalf = lane >> 5;
-  const int rr = min(lrow, rows - 1);
-  const int qi = small_div(rr, 1.0f / (float)g);
-  const int hq = kvh * g + (rr - qi * g);
+  const int q0 = it.tile * kFew / g, h0 = it.tile * kFew - q0 * g;  // of the tile's first row
+  const int rr = h0 + min(lrow, rows - 1);
+  const int dq = small_div(rr, 1.0f / (float)g);
+  const int qi = q0 + dq;
+  const int hq = kvh * g + (rr - dq * g);
   u32x4_t qf[8];
   {
     const char* qp = a.q + (int64_t)(it.qbase + qi) * a.q_ld + (int64_t)hq * kRowB;
@@ -582,7 +596,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     }
   }
   const int vis = row_limit(a, it, qi, kend);              // keys [0, vis) are seen
-  const int vis0 = row_limit(a, it, 0, kend);              // by the first row
+  const int vis0 = row_limit(a, it, q0, kend);             // by the first row
   const int vis1 = min(it.vis_end, kend);                  // and by the last
 
   char* const vt = smem + wave * (kF8 ? kVTile : 2 * kVTile);  // bf16: K tile, then V tile
@@ -825,19 +839,19 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   const float vs = kF8 && a.vs ? a.vs[kvh] : 1.0f;
   // thread: rows tid / 32 (+ 8, 16, 24), dims 4 (tid % 32) .. +3
   const int qd = tid_e & 31, r_first = tid_e >> 5;
-  const __amdgpu_buffer_rsrc_t prs = part_rsrc(a);
+  const __amdgpu_buffer_rsrc_t prs = part_rsrc<kDecode>(a);
   auto finish = [&](int r, const f32x4_t& x, float l) __attribute__((always_inline)) {
-    const int q2 = small_div(r, 1.0f / (float)g);
-    const float inv = normalizer(l, vs, row_limit(a, it, q2, it.nk) > 0);
-    store4<true>(a.o + ((int64_t)(it.qbase + q2) * a.H + kvh * g + (r - q2 * g)) * kRowB + 8 * qd, x[0] * inv,
+    const int q2 = small_div(h0 + r, 1.0f / (float)g);
+    const float inv = normalizer(l, vs, row_limit(a, it, q0 + q2, it.nk) > 0);
+    store4<true>(a.o + ((int64_t)(it.qbase + q0 + q2) * a.H + kvh * g + (h0 + r - q2 * g)) * kRowB + 8 * qd, x[0] * inv,
                  x[1] * inv, x[2] * inv, x[3] * inv);
   };
   auto keep = [&](int slot, int r, const f32x4_t& x, float m, float l) __attribute__((always_inline)) {
-    const uint32_t at = (uint32_t)slot * kSlotBytes;
+    const uint32_t at = (uint32_t)slot * kSlotBytes<kDecode>;
     part_store4(prs, at + r * (kDh * 4) + qd * 16, x[0], x[1], x[2], x[3]);
     if (qd == 0) {
-      part_store(prs, at + kStats + r * 4, m);
-      part_store(prs, at + kStats + (kPagedRows + r) * 4, l);
+      part_store(prs, at + kStats<kDecode> + r * 4, m);
+      part_store(prs, at + kStats<kDecode> + (kSlotRows<kDecode> + r) * 4, l);
     }
   };
   for (int r = r_first; r < rows; r += 8) {
@@ -855,7 +869,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     else
       finish(r, x, lr);
   }
-  if (!a.meet_in_launch) return;
+  if constexpr (!kDecode) return;
   // ---- the chunks meet, 16 at a time, eight rows at a time; all their loads are in
   //      flight together ----
   int n = it.n_chunks, idx = it.c, stride = 1;
@@ -865,7 +879,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     n = (n + kMeet - 1) / kMeet;
     idx /= kMeet;
     if (size > 1) {
-      if (!arrive_last(a, level * kPagedTarget + slot, size, reinterpret_cast<int*>(ml))) return;
+      if (!arrive_last(a, level * kPagedPlaces + slot, size, reinterpret_cast<int*>(ml))) return;
       int slot_v = slot;
       asm volatile("" : "+v"(slot_v));  // (sixteen offsets in scalar registers are too many)
       for (int rb = 0; rb < rows; rb += 8) {
@@ -874,10 +888,10 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
         float mc[kMeet], lc[kMeet];
 #pragma unroll
         for (int i = 0; i < kMeet; ++i) {
-          const uint32_t at = (uint32_t)(slot_v + min(i, size - 1) * stride) * kSlotBytes;
+          const uint32_t at = (uint32_t)(slot_v + min(i, size - 1) * stride) * kSlotBytes<kDecode>;
           y[i] = part_load4(prs, at + r * (kDh * 4) + qd * 16);
-          mc[i] = part_load(prs, at + kStats + r * 4);
-          lc[i] = part_load(prs, at + kStats + (kPagedRows + r) * 4);
+          mc[i] = part_load(prs, at + kStats<kDecode> + r * 4);
+          lc[i] = part_load(prs, at + kStats<kDecode> + (kSlotRows<kDecode> + r) * 4);
         }
         f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
         float m = -__builtin_inff(), l = 0.0f;
@@ -954,7 +968,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   };
 
   // ---- rows: row r of the sequence is query r / g, head r % g of the group ----
-  const int r0 = it.tile * kPagedRows;
+  const int r0 = it.tile * kTileRows;
   const int q0 = r0 / g;         // first query, and the first row's place in its group
   const int h0 = r0 - q0 * g;
 
@@ -1098,7 +1112,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     constexpr int kPer = 16 / (kHi - kLo);                     // probabilities after each
     u32x4_t fr[16];
 #pragma unroll
-    for (int j = kLo; j < kLo + kAhead; ++j) fr[j] = frag(j, kKb, kVb);
+    for (int j = kLo; j < kLo + kGroup; ++j) fr[j] = frag(j, kKb, kVb);
     // The running maximum moves (and the output is rescaled) only when some
     // lane's block maximum exceeds it by more than kLazy in the exponent, so
     // probabilities stay below 2^kLazy; the sum l uses the same maximum, so
@@ -1118,17 +1132,23 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
       m_run = m_new;
     }
     const float mc = m_run == -__builtin_inff() ? 0.0f : m_run * c2;
-    float rs = 0.0f, even = 0.0f;
-    auto prob = [&](int e) __attribute__((always_inline)) {
-      float p = __builtin_amdgcn_exp2f(fmaf(sc[e], c2, -mc));
-      asm volatile("" : "+v"(p));  // this and the next keep the value between its fences
-      if (e & 1) {
-        rs += even + p;
-        uint32_t w = pack_bf16(even, p);
+    // Step k: exponential k, the exponent of k + 1, and the pair before k is added
+    // and packed; nothing in a step waits for the step's own exponential.
+    float rs = 0.0f, p[16], ex = fmaf(sc[0], c2, -mc);
+    auto soft = [&](int k) __attribute__((always_inline)) {
+      if (k < 16) {
+        p[k] = __builtin_amdgcn_exp2f(ex);
+        asm volatile("" : "+v"(p[k]));  // this and the others keep the values between their fences
+      }
+      if (k < 15) {
+        ex = fmaf(sc[k + 1], c2, -mc);
+        asm volatile("" : "+v"(ex));
+      }
+      if (k >= 2 && !(k & 1)) {
+        rs += p[k - 2] + p[k - 1];
+        uint32_t w = pack_bf16(p[k - 2], p[k - 1]);
         asm volatile("" : "+v"(w), "+v"(rs));
-        pn[e >> 3][(e & 7) >> 1] = w;
-      } else {
-        even = p;
+        pn[(k - 2) >> 3][((k - 2) & 7) >> 1] = w;
       }
     };
     float mx = -__builtin_inff();
@@ -1136,14 +1156,17 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = kLo; j < kHi; ++j) {
-      if (j + kAhead < kHi) fr[j + kAhead] = frag(j + kAhead, kKb, kVb);
+      if (j % kGroup == 0 && j + kGroup < kHi) {
+#pragma unroll
+        for (int i = j + kGroup; i < j + 2 * kGroup; ++i) fr[i] = frag(i, kKb, kVb);
+      }
       if (j == 0) sn = f32x16_t{};
       if (j < 8)
         mfma_step<true>(sn, fr[j], qf[j]);
       else
         mfma_step<true>(oacc[j & 3], fr[j], pp[(j - 8) >> 2]);
 #pragma unroll
-      for (int e = (j - kLo) * kPer; e < (j - kLo + 1) * kPer; ++e) prob(e);
+      for (int k = (j - kLo) * kPer; k < (j - kLo + 1) * kPer; ++k) soft(k);
       if (!kLast && !kFirst && j >= 12) {
 #pragma unroll
         for (int v = 4 * (j - 12); v < 4 * (j - 11); ++v) mx = fmaxf(mx, sn[v]);
@@ -1151,6 +1174,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
+    soft(16);
     l_run += rs;
     if constexpr (!kFirst) {
       if (move) {
@@ -1279,15 +1303,15 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   l_run += __shfl_xor(l_run, 32);
   if (it.n_chunks > 1) {
     // ---- partial results, as the lanes hold them, for paged_combine_kernel ----
-    float* const p = a.part + (int64_t)(it.slot + it.c) * kPagedPart;
+    float* const p = a.part + (int64_t)(it.slot + it.c) * (kSlotBytes<false> / 4);
 #pragma unroll
     for (int v = 0; v < 16; ++v)
       *reinterpret_cast<f32x4_t*>(p + ((wave * 16 + v) * 64 + lane) * 4) =
           f32x4_t{oacc[v >> 2][4 * (v & 3)], oacc[v >> 2][4 * (v & 3) + 1], oacc[v >> 2][4 * (v & 3) + 2],
                   oacc[v >> 2][4 * (v & 3) + 3]};
     if (lhalf == 0) {
-      p[kPagedRows * kDh + 32 * wave + lrow] = m_run;
-      p[kPagedRows * kDh + kPagedRows + 32 * wave + lrow] = l_run;
+      p[kTileRows * kDh + 32 * wave + lrow] = m_run;
+      p[kTileRows * (kDh + 1) + 32 * wave + lrow] = l_run;
     }
     return;
   }

@@ -109,7 +109,7 @@ def test_row_strides():
     assert append(cache(), kld=255) == append(cache(), vld=252) == append(cache(), kld=128) == INV
     assert append(cache(), kld=1 << 31) == append(cache(), vld=1 << 31) == UNS
     assert attend(cache(), attn(), ld=12 * 128 - 8) == attend(cache(), attn(), ld=12 * 128 + 4) == INV
-    assert attend(cache(), attn(), ld=1 << 23) == UNS
+    assert attend(cache(), attn(), ld=1 << 22) == UNS
 
 
 def test_workspace():
