@@ -260,7 +260,7 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
   p.items = units;
   if (B > kPagedScan) p.plan_bytes = ((size_t)(B + 1) * sizeof(PagedPlan) + 255) / 256 * 256;
   p.bytes = p.plan_bytes;
-  if (max_keys >= 2 * kMinFew) {  // else nothing is cut
+  if (max_keys >= 2 * kMinTile) {  // else nothing is cut
     p.items += kPagedPlaces;
     if (p.decode)
       p.count_bytes = (size_t)kPagedLevels * kPagedPlaces * sizeof(unsigned long long);

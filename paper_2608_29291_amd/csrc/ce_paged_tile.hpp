@@ -21,6 +21,9 @@ constexpr int kKBytes = kKT * kRowB;
 constexpr int kGroup = 4;          // MFMA operands read from LDS together, one group ahead
 constexpr float kLazy = 8.0f;      // headroom of the running maximum (exponent of 2)
 constexpr int kMinFew = 128;       // least keys of a chunk: one tile of 32 for each wave
+constexpr int kWholeFew = 640;     // least keys of a sequence that is cut for a few rows
+constexpr int kMaxHalf = 1024;     // keys per place up to which single tokens fill half of the places
+constexpr int kMaxMeet = 512;      // keys per chunk up to which no more than kMeet meet
 constexpr int kMinTile = 256;
 constexpr int kMeet = 16;          // chunks that meet at a time in the launch itself
 constexpr int kOLd = kDh + 4;      // floats per row of paged_few's outputs in LDS
@@ -28,6 +31,7 @@ constexpr int kVRow = kBK * 2;     // bytes per row of paged_few's V^T
 constexpr int kVTile = kDh * kVRow;
 constexpr int kSmem = 4 * kFew * kOLd * 4 + 2 * 4 * kFew * 4;
 static_assert(kSmem >= 4 * 2 * kVTile && kSmem >= 4 * kKBytes && 2 * kSmem <= 160 * 1024, "the tiles fit");
+static_assert(kWholeFew >= 2 * kMinTile, "the host takes 2 kMinTile keys for the least that is cut");
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
@@ -49,7 +53,15 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 //     places, every unit may be cut, L = A.
 // A unit of n_k keys is cut into floor(n_k / L) chunks, so the chunks of all cut units
 // are at most S (a second round of a few would double the time) and as many
-// partial results fit the workspace.
+// partial results fit the workspace. A few rows are cut less than that where it does
+// not pay (us, single tokens at 28 / 4 heads, bf16, before / after):
+//   * below 640 keys not at all: 1 x 300 keys 9.7 / 7.5, 32 x 600 14.9 / 11.1;
+//   * into at most 16 chunks, that meet at once, as long as these have no more than 512
+//     keys: 1 x 4000 13.0 / 10.6, 8 x 5 drafted tokens over 333 to 4103 18.3 / 15.9;
+//   * single tokens into half as many where a place's share is at most 1024 keys: one
+//     workgroup a CU keeps the memory as busy, and fewer chunks meet: 16 sequences of
+//     551 to 3100 16.4 / 15.3, 32 x 1000 18.2 / 14.8. Above, unequal sequences need the
+//     finer cut: 64 of 2100 to 16001 keys, 8 bits, 78 (half as many: 114).
 //
 // How the chunks meet: of single tokens, in the launch itself (a second one would
 // cost 5 us of 18); of many rows, by a second launch over the whole chip, since one
@@ -91,7 +103,13 @@ __device__ __forceinline__ int chunk_length(float w) {
 // A sequence's chunks (a whole number of its waves' tiles).
 __device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, int& C, int& chunk) {
   const bool few = is_few(a, s.nq, g);
-  C = s.nk / (few ? max(2 * min(L, 1 << 29), kMinFew) : max(L, kMinTile));
+  if (few) {
+    const int l = 2 * min(L, 1 << 28);
+    C = s.nk < kWholeFew ? 1 : s.nk / max(a.decode && l <= kMaxHalf ? 2 * l : l, kMinFew);
+    if (C > kMeet && s.nk <= kMeet * kMaxMeet) C = kMeet;
+  } else {
+    C = s.nk / max(L, kMinTile);
+  }
   chunk = s.nk;
   if (C > 1) {
     const int unit = few ? kBK : kKT;

@@ -77,6 +77,27 @@ def test_long_cache(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_long_caches_of_single_tokens(dtype):
+    """More than 16 chunks: they meet in two levels, in groups of 16 and a rest."""
+    lens = [20011, 9000, 8193, 1]
+    p = U.Paged(lens, 1, 16, dtype, seed=5)
+    q = rows([1] * 4, 7)
+    U.check(U.attend(p, q, [1] * 4, True), *p.answer(q, [1] * 4, True, U.DH ** -0.5))
+
+
+def test_more_than_256_chunks_of_one_token():
+    """Three levels: one head over 600000 keys, the same 32 pages over and over."""
+    p = U.Paged([32 * 256], 1, 256, "bf16", seed=6)
+    times = 600000 // (32 * 256) + 1
+    p.table = np.concatenate([np.tile(p.table[:, :32], (1, times)), p.table[:, 32:]], 1)
+    p.lens = [600000]
+    p.k_used, p.v_used = ([np.tile(x[0], (times, 1, 1))[:600000]] for x in (p.k, p.v))
+    q = rows([1], 3, spread=3.0)
+    got, (want, top) = U.attend(p, q, [1], True), p.answer(q, [1], True, U.DH ** -0.5)
+    U.check(got, want, top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 40])
 def test_shared_pages_and_long_chunks(n, dtype):
     """So many sequences over one long prefix that none is cut: a workgroup's keys run
