@@ -50,7 +50,7 @@ enum {
  *   page_table   device int32 [B x max_pages]; entries behind a sequence's last
  *                page are not read
  * Limits: head_dim 128; page_size a power of two from 16 to 256; n_pages *
- * page_size and max_pages * page_size below 2^31; 1 <= B <= 65535.
+ * page_size below 2^31, max_pages * page_size at most 2^30; 1 <= B <= 65535.
  */
 typedef struct ce_kv_cache {
   int32_t B;
@@ -96,8 +96,11 @@ typedef struct ce_kv_cache {
  *   slots       device int32 [row_capacity] out: slot of each row; -1 for rows of
  *               refused sequences and rows behind the last
  *   status      device uint32 [1] out or NULL: CE_DEV_* bits of this call
- * Deterministic. Errors: CE_ERR_INVALID_ARG for null pointers / sizes,
- * CE_ERR_UNSUPPORTED outside the limits, CE_ERR_HIP.
+ * Calls on one pool change it and must not overlap. Deterministic, but where the
+ * offsets are out of order (CE_DEV_BAD_OFFSETS): a row that lies in the ranges of
+ * several sequences then has the slot of one of them. Errors:
+ * CE_ERR_INVALID_ARG for null pointers / sizes, CE_ERR_UNSUPPORTED outside the
+ * limits, CE_ERR_HIP.
  */
 int ce_kv_reserve(const ce_kv_cache* cache, const int32_t* lens, const int32_t* new_offsets, int32_t row_capacity,
                   const uint8_t* reset, int32_t* free_pages, const int32_t* free_count, int32_t* lens_out,
@@ -109,8 +112,8 @@ int ce_kv_reserve(const ce_kv_cache* cache, const int32_t* lens, const int32_t* 
  *                 head_dim values contiguous (a part of a fused projection's rows);
  *                 k_ld, v_ld multiples of 8
  *   slots         device int32 [rows]: ce_kv_reserve's; rows whose slot is outside
- *                 [0, n_pages * page_size) are skipped. Of rows with the same slot any
- *                 one is stored
+ *                 [0, n_pages * page_size) are skipped. Rows with the same slot race:
+ *                 each 16 bytes of the page are one row's
  * CE_BF16 pages take the values as they are, CE_E4M3 pages x / scale (one float32
  * division) limited to +-448 and rounded to nearest even; NaN stays NaN.
  * The page table is not read. Errors as ce_kv_reserve.
@@ -146,10 +149,10 @@ typedef struct ce_paged_attn {
  * Lengths are clamped to [0, max_pages * page_size]; a page number outside
  * [0, n_pages) reads as zeros. fp32 scores, statistics and accumulation; the
  * probabilities are rounded to bf16 for the product with V. Deterministic.
- * Errors: CE_ERR_INVALID_ARG for null pointers, sizes, a scale that is not a
- * positive finite number or causal outside {0, 1}; CE_ERR_UNSUPPORTED outside
+ * Errors: CE_ERR_INVALID_ARG for null pointers, sizes, a scale that is not
+ * positive with scale * log2 e finite or causal outside {0, 1}; CE_ERR_UNSUPPORTED outside
  * the limits, for more than 4096 query heads a key/value head, q_capacity * n_heads
- * >= 2^29 or B * n_kv_heads >= 2^22;
+ * >= 2^28 or B * n_kv_heads >= 2^22;
  * CE_ERR_WORKSPACE; CE_ERR_HIP.
  * ce_paged_workspace_size depends on the sizes in cache and attn only (no device
  * pointer is read), is at most 35 MB, and 0 where none is used or the call

@@ -810,7 +810,7 @@ def _rows3(x, name, d, heads=None):
         p = x.data_ptr()
         if (x.dtype is torch.bfloat16 and x.get_device() == _device() and dx == d and (heads is None or h == heads)
                 and st[1:] == (d, 1) and st[0] >= h * d and not (st[0] | p >> 1) & 7):
-            return p, n, h, st[0]
+            return p, n, h, st[0] if n > 1 else h * d
     except (AttributeError, TypeError, ValueError):
         pass
     if x is None or x.dim() != 3 or x.shape[2] != d or (heads is not None and x.shape[1] != heads):

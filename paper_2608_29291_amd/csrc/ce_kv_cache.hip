@@ -214,17 +214,18 @@ __global__ __launch_bounds__(1024) void kv_reserve_kernel(ReserveArgs a) {
 }
 
 // Slots of many rows, after kv_reserve_kernel: the workgroups (b, *) walk the
-// rows of sequence b, and all of them the rows behind the last.
+// rows of sequence b, and all of them the rows behind the last (and before the
+// first, where the offsets are wrong).
 __global__ __launch_bounds__(256) void kv_slots_kernel(ReserveArgs a) {
   const int b = blockIdx.x;
   const int lo = clampi(a.offs[b], 0, a.rows);
   const int hi = clampi(a.offs[b + 1], lo, a.rows);
   const int start = a.start[b];
   const int mask = (1 << a.page_log2) - 1;
-  for (int r = lo + blockIdx.y * 256 + threadIdx.x; r < hi; r += gridDim.y * 256) {
+  for (int64_t r = lo + (int64_t)blockIdx.y * 256 + threadIdx.x; r < hi; r += gridDim.y * 256) {
     int slot = -1;
     if (start >= 0) {
-      const int t = start + (r - lo);
+      const int t = start + (int)(r - lo);
       const int page = a.table[(int64_t)b * a.max_pages + (t >> a.page_log2)];
       if ((uint32_t)page < (uint32_t)a.n_pages) slot = (page << a.page_log2) + (t & mask);
     }
@@ -232,7 +233,10 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(ReserveArgs a) {
   }
   const int end = clampi(a.offs[a.B], 0, a.rows);
   const int64_t all = (int64_t)gridDim.x * gridDim.y * 256;
-  for (int64_t r = end + ((int64_t)blockIdx.y * gridDim.x + b) * 256 + threadIdx.x; r < a.rows; r += all) a.slots[r] = -1;
+  const int64_t at = ((int64_t)blockIdx.y * gridDim.x + b) * 256 + threadIdx.x;
+  for (int64_t r = end + at; r < a.rows; r += all) a.slots[r] = -1;
+  const int begin = clampi(a.offs[0], 0, a.rows);
+  for (int64_t r = at; r < begin; r += all) a.slots[r] = -1;
 }
 
 // 8 bf16 (a 16-byte load) / scale, limited to +-448, as 8 bytes of e4m3. The quotient
@@ -240,8 +244,9 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(ReserveArgs a) {
 // q + (x - q scale) r, the remainder by one fma, is x / scale rounded to nearest
 // (Markstein), in three instructions instead of the ten of a division that provides
 // for every exponent. Quotients past 500, which are limited anyway, infinities,
-// NaN and zeros (of either sign) keep q. kDivide: the division, for scales whose
-// products leave the exponents' middle.
+// NaN and zeros (of either sign) keep q. kDivide: the division, for scales outside
+// 1e-24 .. 1e24: the remainder of a value that is not rounded to zero reaches 2^-57 of
+// the scale, which has to be a normal float.
 template <bool kDivide>
 __device__ __forceinline__ u32x2_t to_e4m3(const u32x4_t& x, float scale, float r) {
   float f[8];
@@ -278,9 +283,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   constexpr int kLoad = kE4m3 ? 2 : 1;  // 16-byte loads of a piece
   const uint32_t half = (uint32_t)a.Hkv * kPer;  // pieces of a row of K, and of V
   const uint32_t n = (uint32_t)a.rows_per_block * 2 * half;
+  const int64_t row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.rows_per_block;
   for (uint32_t i = threadIdx.x; i < n; i += 256) {
     const uint32_t rl = i / (2 * half);
-    const int r = (int)blockIdx.x * a.rows_per_block + (int)rl;
+    const int64_t r = row0 + rl;
     if (r >= a.rows) break;
     uint32_t c = i - rl * 2 * half;
     const int slot = a.slots[r];
@@ -288,7 +294,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     const bool is_v = c >= half;
     if (is_v) c -= half;
     const uint32_t h = c / kPer;
-    const char* src = (is_v ? a.v_new + (int64_t)r * a.v_ld : a.k_new + (int64_t)r * a.k_ld) + (int64_t)c * (16 * kLoad);
+    const char* src = (is_v ? a.v_new + r * a.v_ld : a.k_new + r * a.k_ld) + (int64_t)c * (16 * kLoad);
     char* dst = (is_v ? a.v : a.k) + (int64_t)((uint64_t)(uint32_t)(slot >> a.page_log2) * a.page_bytes) +
                 (((int64_t)h << a.page_log2) + (slot & ((1 << a.page_log2) - 1))) * kRow + (c & (kPer - 1)) * 16;
     const u32x4_t x = gload16_cached(src);
@@ -297,7 +303,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
       const float* const sc = is_v ? a.v_scale : a.k_scale;
       const float s = sc ? sc[h] : 1.0f;
       u32x2_t p, q;
-      if (__builtin_amdgcn_ballot_w64(!(s > 1e-30f && s < 1e30f))) {
+      if (__builtin_amdgcn_ballot_w64(!(s > 1e-24f && s < 1e24f))) {
         p = to_e4m3<true>(x, s, 0.0f);
         q = to_e4m3<true>(y, s, 0.0f);
       } else {
@@ -337,11 +343,13 @@ hipError_t launch_kv_append(AppendArgs a, bool e4m3, hipStream_t stream) {
   const int64_t pieces = (int64_t)2 * a.Hkv * (e4m3 ? 8 : 16);
   const int64_t per = 256 / pieces;
   a.rows_per_block = per < 1 ? 1 : (int)per;
-  const int grid = (a.rows + a.rows_per_block - 1) / a.rows_per_block;
+  const int64_t blocks = ((int64_t)a.rows + a.rows_per_block - 1) / a.rows_per_block;
+  const int64_t x = blocks < 1 << 16 ? blocks : 1 << 16;
+  const dim3 grid((unsigned)x, (unsigned)((blocks + x - 1) / x));
   if (e4m3)
-    hipLaunchKernelGGL(kv_append_kernel<true>, dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(kv_append_kernel<true>, grid, dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL(kv_append_kernel<false>, dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(kv_append_kernel<false>, grid, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -24,7 +24,8 @@ int check_table(const ce_kv_cache* c) {
   if (c->B > 65535 || c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)))
     return CE_ERR_UNSUPPORTED;
   const int64_t lim = (int64_t)1 << 31;
-  if ((int64_t)c->n_pages * c->page_size >= lim || (int64_t)c->max_pages * c->page_size >= lim) return CE_ERR_UNSUPPORTED;
+  if ((int64_t)c->n_pages * c->page_size >= lim || (int64_t)c->max_pages * c->page_size > lim / 2)
+    return CE_ERR_UNSUPPORTED;
   return CE_OK;
 }
 
@@ -48,8 +49,8 @@ int check_attn(const ce_kv_cache* c, const ce_paged_attn* at) {
   if (!at || at->n_heads < 1 || at->n_heads % c->n_kv_heads != 0 || at->q_capacity < 0) return CE_ERR_INVALID_ARG;
   if (at->n_heads / c->n_kv_heads > 4096) return CE_ERR_UNSUPPORTED;
   if (at->causal != 0 && at->causal != 1) return CE_ERR_INVALID_ARG;
-  if (!isfinite(at->scale) || !(at->scale > 0.0f)) return CE_ERR_INVALID_ARG;
-  if ((int64_t)at->q_capacity * at->n_heads >= (int64_t)1 << 29 || (int64_t)c->B * c->n_kv_heads >= (int64_t)1 << 22)
+  if (!(at->scale > 0.0f) || !isfinite(at->scale * 1.4426950408889634f)) return CE_ERR_INVALID_ARG;
+  if ((int64_t)at->q_capacity * at->n_heads >= (int64_t)1 << 28 || (int64_t)c->B * c->n_kv_heads >= (int64_t)1 << 22)
     return CE_ERR_UNSUPPORTED;
   return CE_OK;
 }

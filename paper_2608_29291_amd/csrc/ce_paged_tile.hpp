@@ -104,7 +104,7 @@ __device__ __forceinline__ int chunk_length(float w) {
 __device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, int& C, int& chunk) {
   const bool few = is_few(a, s.nq, g);
   if (few) {
-    const int l = 2 * min(L, 1 << 28);
+    const int l = 2 * min(L, 1 << 29);  // (2^30: nothing is cut)
     C = s.nk < kWholeFew ? 1 : s.nk / max(a.decode && l <= kMaxHalf ? 2 * l : l, kMinFew);
     if (C > kMeet && s.nk <= kMeet * kMaxMeet) C = kMeet;
   } else {

@@ -40,13 +40,14 @@ def attn(**kw):
 INV, UNS, WS = -1, -2, -3
 TABLE = [({"B": 0}, INV), ({"page_size": 0}, INV), ({"n_pages": 0}, INV), ({"max_pages": 0}, INV), ({"B": 65536}, UNS),
          ({"page_size": 8}, UNS), ({"page_size": 48}, UNS), ({"page_size": 512}, UNS), ({"n_pages": 1 << 27}, UNS),
-         ({"max_pages": 1 << 27}, UNS)]
+         ({"max_pages": (1 << 26) + 1}, UNS)]
 PAGES = [({"n_kv_heads": 0}, INV), ({"head_dim": 64}, UNS), ({"dtype": ce.CE_F32}, UNS), ({"dtype": 3}, UNS),
          ({"page_stride": 2 * 16 * 128 - 16}, INV), ({"page_stride": 2 * 16 * 128 + 8}, INV),
          ({"page_stride": 1 << 31}, UNS), ({"k_scale": FAKE}, INV), ({"k_scale": FAKE, "v_scale": FAKE}, INV),
          ({"dtype": ce.CE_E4M3, "v_scale": FAKE}, INV), ({"n_kv_heads": 1 << 16, "page_stride": 1 << 28}, UNS)]
 ATTN = [({"n_heads": 0}, INV), ({"n_heads": 13}, INV), ({"q_capacity": -1}, INV), ({"causal": 2}, INV),
         ({"scale": 0.0}, INV), ({"scale": -1.0}, INV), ({"scale": float("nan")}, INV), ({"scale": float("inf")}, INV),
+        ({"scale": 3e38}, INV), ({"n_heads": 2 * 4097}, UNS),
         ({"q_capacity": 1 << 26}, UNS)]
 
 
