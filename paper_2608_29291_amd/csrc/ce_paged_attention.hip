@@ -14,6 +14,10 @@
 // the rows). Grouped rows waste less than one tile per query head: 551 queries of
 // six heads are 26 tiles, not 30, and the tile's causal edge is g times as steep.
 //
+// A call of single tokens (no more rows than sequences, at most eight heads a key/value
+// head) is a launch of its own in which all rows go 32 to a tile (paged_decode_kernel),
+// with half the partial results and without the second launch.
+//
 // Keys. Tiles are cut along their keys, too, where they leave places on the chip idle
 // (the plan: ce_paged_tile.hpp). Every wave forms the plan by itself from the
 // lengths, which only the device knows: a lane per sequence, or per four, and a few
@@ -162,7 +166,9 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
   }
 }
 
-// Partial results of the cut units, in chunk order. Workgroup (unit, z): 32 rows z of
+// Partial results of the cut units, in chunk order. Bound: latency, 5 us with the plan
+// for 8 x 5 rows and 8 for 512 queries over 8704 keys, whose 29 MB come from the
+// caches. Workgroup (unit, z): 32 rows z of
 // a 128-row tile, as wave z of its chunks' workgroups left them; of a few rows, eight.
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
   Item it;
