@@ -48,20 +48,22 @@ struct PagedArgs {
   const int32_t *table, *qo, *lens;
   int64_t q_ld;        // bytes between rows of q
   uint32_t page_bytes;  // bytes between pages
-  int B, H, Hkv, q_cap, n_pages, max_pages, page_log2, causal;
+  int B, H, Hkv, g, q_cap, n_pages, max_pages, page_log2, causal;
   float scale_log2;  // scale * log2(e)
   int decode;        // a call of single tokens (the plan: ce_paged_tile.hpp)
   uint32_t grid;     // items that the launch has workgroups for
   float* part;       // partial results, a slot for each place
-  unsigned long long* arrived;  // counters of the chunks that meet, kPagedPlaces a level
+  unsigned long long* arrived;  // single tokens: counters of the chunks that meet, kPagedPlaces a level
+  uint32_t* units;   // else the number of cut units and a record of each, or NULL: none is cut
   unsigned long long token;     // of this call, 48 bits
-  PagedPlan* plan;   // B > kPagedScan: the sequences, then the totals and (whole) the chunk length
+  PagedPlan* plan;   // B > kPagedScan: the sequences, then the items and (whole) the chunk length
 };
 
 constexpr int kPagedScan = 256;    // sequences that a wave plans by itself (four a lane)
 constexpr int kPagedFew = 32;     // (query, head) rows of a tile of single tokens
 constexpr int kPagedTile = 128;   // and of one of many rows
 constexpr int kPagedPlaces = 512; // places for workgroups: two on each CU
+constexpr int kPagedRecord = 32;  // bytes of a cut unit's record
 constexpr int kPagedLevels = 3;    // sixteen chunks meet at a time, 512 at most
 
 // What the host knows of a call: the workgroups that any batch of these sizes needs.
@@ -69,7 +71,7 @@ struct PagedGrid {
   int64_t items;
   int decode;
   int cut_units;  // for the launch that adds chunks up, at most (0: no such launch)
-  size_t plan_bytes, count_bytes, bytes;  // workspace: the plan, arrival counters, partial results
+  size_t plan_bytes, count_bytes, bytes;  // workspace: the plan, counters or records, partial results
 };
 PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys);
 

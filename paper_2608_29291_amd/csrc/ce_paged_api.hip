@@ -153,6 +153,7 @@ int ce_paged_attention(const ce_kv_cache* cache, const ce_paged_attn* attn, cons
   a.B = cache->B;
   a.H = attn->n_heads;
   a.Hkv = cache->n_kv_heads;
+  a.g = a.H / a.Hkv;
   a.q_cap = attn->q_capacity;
   a.n_pages = cache->n_pages;
   a.max_pages = cache->max_pages;
@@ -162,6 +163,7 @@ int ce_paged_attention(const ce_kv_cache* cache, const ce_paged_attn* attn, cons
   char* const w = static_cast<char*>(ws);
   a.plan = reinterpret_cast<PagedPlan*>(w);
   a.arrived = reinterpret_cast<unsigned long long*>(w + p.plan_bytes);
+  a.units = p.cut_units ? reinterpret_cast<uint32_t*>(w + p.plan_bytes) : nullptr;
   a.part = reinterpret_cast<float*>(w + p.plan_bytes + p.count_bytes);
   return hip_status(launch_paged_attention(a, cache->dtype == CE_E4M3, static_cast<hipStream_t>(stream)));
 }

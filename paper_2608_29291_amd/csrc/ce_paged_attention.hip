@@ -62,7 +62,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                                                                                                         uint32_t group) {
   __shared__ __attribute__((aligned(1024))) char smem[kSmem];
   Item it;
-  if (!find_item<false>(a, item_of(blockIdx.x, group), it)) return;
+  if (!find_item<true>(a, item_of(blockIdx.x, group), it)) return;
+  if (it.record >= 0 && it.c == 0 && threadIdx.x == 0) write_record(a, it);
   if (it.few)
     paged_few<kF8, false>(a, smem, it);
   else
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
   __shared__ float wsum[8];
   __shared__ float wmax[8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int g = a.H / a.Hkv;
+  const int g = a.g;
   // exclusive prefix sum over the threads, and the total
   auto scan = [&](int64_t v, int64_t& total) {
     int64_t x = v;
@@ -157,8 +158,8 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
     }
     if (tid == 0) {
       a.plan[a.B].items = put(items);
-      a.plan[a.B].cut = put(cuts);
       a.plan[a.B].whole = (uint32_t)L;
+      if (a.units) *a.units = put(cuts);
     }
     // (as in find_by_scan)
     if (L == 1 << 30 || (items <= a.grid && slots <= kPagedPlaces)) break;
@@ -172,9 +173,10 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
 // a 128-row tile, as wave z of its chunks' workgroups left them; of a few rows, eight.
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
   Item it;
-  if (!find_item<true>(a, blockIdx.x, it) || it.n_chunks <= 1) return;
+  read_record(a, blockIdx.x, it);  // (any content behind the last, and not used)
+  if (blockIdx.x >= *a.units || it.n_chunks <= 1) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int g = a.H / a.Hkv;
+  const int g = a.g;
   const int n = it.n_chunks;
   const float c2 = a.scale_log2 * (a.ks ? a.ks[it.kvh] : 1.0f);
   const float vs = a.vs ? a.vs[it.kvh] : 1.0f;
@@ -268,10 +270,12 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
   p.bytes = p.plan_bytes;
   if (max_keys >= 2 * kMinTile) {  // else nothing is cut
     p.items += kPagedPlaces;
-    if (p.decode)
+    if (p.decode) {
       p.count_bytes = (size_t)kPagedLevels * kPagedPlaces * sizeof(unsigned long long);
-    else  // a cut unit has two chunks at least
+    } else {  // a cut unit has two chunks at least
       p.cut_units = (int)(units < kPagedPlaces / 2 ? units : kPagedPlaces / 2);
+      p.count_bytes = ((size_t)(kPagedPlaces / 2 + 1) * kPagedRecord + 255) / 256 * 256;
+    }
     p.bytes += p.count_bytes + (size_t)kPagedPlaces * (p.decode ? kSlotBytes<true> : kSlotBytes<false>);
   }
   return p;

@@ -15,6 +15,8 @@ constexpr int kDh = 128;           // head dimension
 constexpr int kRowB = kDh * 2;     // bytes of a bf16 row
 constexpr int kFew = kPagedFew;
 constexpr int kTileRows = kPagedTile;
+constexpr int kFewLog2 = 5, kTileLog2 = 7;
+static_assert(kFew == 1 << kFewLog2 && kTileRows == 1 << kTileLog2, "rows of the tiles");
 constexpr int kKT = 64;            // keys per tile of paged_tile
 constexpr int kBK = 32;            // keys per block: one pass of the softmax
 constexpr int kKBytes = kKT * kRowB;
@@ -80,8 +82,8 @@ __device__ __forceinline__ Size size_from(const PagedArgs& a, int q0, int q1, in
   s.qbase = clampi(q0, 0, a.q_cap);
   s.nq = clampi(q1, s.qbase, a.q_cap) - s.qbase;
   s.nk = clampi(len, 0, a.max_pages << a.page_log2);
-  const int rows = tile_rows(is_few(a, s.nq, g));
-  s.tiles = (s.nq * g + rows - 1) / rows;
+  const int few = is_few(a, s.nq, g);
+  s.tiles = (s.nq * g + tile_rows(few) - 1) >> (few ? kFewLog2 : kTileLog2);
   return s;
 }
 
@@ -133,18 +135,18 @@ __device__ __forceinline__ float cost_of(const PagedArgs& a, const Size& s, int 
   return (float)s.nk * (is_few(a, s.nq, g) ? 0.5f : 1.0f);
 }
 
-// Its items, its partial results and the units that have such.
+// Its items, its partial results, the units that have such and their chunks.
 struct Counts {
   uint32_t items, slots, cut;
+  int C, chunk;
 };
 __device__ __forceinline__ Counts counts_of(const PagedArgs& a, const Size& s, int g, int L, uint32_t whole) {
-  int C, chunk;
-  cut(a, s, g, L, C, chunk);
-  const uint32_t n = (uint32_t)s.tiles * a.Hkv;
   Counts c;
-  c.cut = C > 1 ? n - whole : 0;
-  c.slots = c.cut * C;
-  c.items = C > 1 ? whole + c.slots : n;
+  cut(a, s, g, L, c.C, c.chunk);
+  const uint32_t n = (uint32_t)s.tiles * a.Hkv;
+  c.cut = c.C > 1 ? n - whole : 0;
+  c.slots = c.cut * c.C;
+  c.items = c.C > 1 ? whole + c.slots : n;
   return c;
 }
 
@@ -154,6 +156,7 @@ struct Item {
   int tile, chunk;   // row tile, keys per chunk
   int c, n_chunks;   // chunk of this item, of those that hold keys its rows see (1: no partial results)
   int slot;          // partial result of its first chunk
+  int record;        // its unit's number among the cut ones, or -1
   int rows;          // rows of the tile
   int vis_end;       // keys that its last row sees
 };
@@ -202,18 +205,19 @@ __device__ __forceinline__ float wave_max(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_readlane(v, 63));
 }
 
-// The sequence that holds an item (or a cut unit), and what was counted before it.
+// The sequence that holds an item, and what was counted before it.
 struct Found {
-  int b, L;
+  int b;
   Size size;
-  uint32_t whole;         // its units that stay whole
-  uint32_t before, slots; // items (or cut units) and partial results of the sequences before
+  int C, chunk;                // its chunks, of keys
+  uint32_t whole;              // its units that stay whole
+  uint32_t before, slots, cut; // items, partial results and cut units of the sequences before
 };
 
-// The sequence of item `at` (kCut: of cut unit `at`); false past the last. Every wave
-// finds it by itself, kPer sequences a lane.
-template <int kPer, bool kCut>
-__device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t at, Found& f) {
+// The sequence of item `at`; false past the last. Every wave finds it by itself, kPer
+// sequences a lane. kRecord: f.cut and, past the last item too, all cut units (n_cut).
+template <int kPer, bool kRecord>
+__device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t at, Found& f, uint32_t& n_cut) {
   const int lane = threadIdx.x & 63;
   Size s[kPer];
   float w = 0.0f, most = 0.0f;
@@ -244,42 +248,46 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
     }
     w = wave_sum(rest);
   }
-  f.L = chunk_length(w);
-  uint32_t count[kPer], slots[kPer], wh[kPer], sum, sum_s, to, slots_to;
+  int L = chunk_length(w);
+  Counts n[kPer];
+  uint32_t wh[kPer], sum, sum_s, sum_c, to, slots_to;
   for (;;) {
-    uint32_t items = 0, first = units_to - units;
-    sum = sum_s = 0;
+    uint32_t first = units_to - units;
+    sum = sum_s = sum_c = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       wh[i] = whole_of(a, s[i], first, whole);
-      const Counts c = counts_of(a, s[i], g, f.L, wh[i]);
+      n[i] = counts_of(a, s[i], g, L, wh[i]);
       first += (uint32_t)s[i].tiles * a.Hkv;
-      count[i] = kCut ? c.cut : c.items;
-      slots[i] = c.slots;
-      items += c.items;
-      sum += count[i];
-      sum_s += slots[i];
+      sum += n[i].items;
+      sum_s += n[i].slots;
+      sum_c += n[i].cut;
     }
     slots_to = wave_scan(sum_s);
     to = wave_scan(sum);
-    const uint32_t items_all = __builtin_amdgcn_readlane(kCut ? wave_scan(items) : to, 63);
     // more workgroups than the launch has, or slots than the workspace: only where
     // offsets are out of order. Then nothing is cut (every chunk of a cut unit
     // must run) and what lies past the grid is left.
-    if (f.L == 1 << 30 ||
-        (items_all <= a.grid && __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedPlaces))
+    if (L == 1 << 30 ||
+        (__builtin_amdgcn_readlane(to, 63) <= a.grid && __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedPlaces))
       break;
-    f.L = 1 << 30;
+    L = 1 << 30;
+  }
+  uint32_t cut_to = 0;
+  if (kRecord && a.units) {
+    cut_to = wave_scan(sum_c);
+    n_cut = __builtin_amdgcn_readlane(cut_to, 63);
   }
   const uint64_t past = __builtin_amdgcn_ballot_w64(at < to);
   if (!past) return false;
   const int ln = __builtin_ctzll(past);
   f.before = __builtin_amdgcn_readlane(to - sum, ln);
   f.slots = __builtin_amdgcn_readlane(slots_to - sum_s, ln);
+  f.cut = __builtin_amdgcn_readlane(cut_to - sum_c, ln);
   bool found = false;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const uint32_t ni = __builtin_amdgcn_readlane(count[i], ln);
+    const uint32_t ni = __builtin_amdgcn_readlane(n[i].items, ln);
     if (found) continue;
     if (i == kPer - 1 || at < f.before + ni) {
       found = true;
@@ -289,19 +297,21 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
       f.size.nk = __builtin_amdgcn_readlane(s[i].nk, ln);
       f.size.tiles = __builtin_amdgcn_readlane(s[i].tiles, ln);
       f.whole = __builtin_amdgcn_readlane(wh[i], ln);
+      f.C = __builtin_amdgcn_readlane(n[i].C, ln);
+      f.chunk = __builtin_amdgcn_readlane(n[i].chunk, ln);
     } else {
       f.before += ni;
-      f.slots += __builtin_amdgcn_readlane(slots[i], ln);
+      f.slots += __builtin_amdgcn_readlane(n[i].slots, ln);
+      f.cut += __builtin_amdgcn_readlane(n[i].cut, ln);
     }
   }
   return true;
 }
 
 // The same from the plan in memory: three rounds of 64 samples.
-template <bool kCut>
 __device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, uint32_t at, Found& f) {
   const int lane = threadIdx.x & 63;
-  auto key = [&](int b) __attribute__((always_inline)) { return kCut ? a.plan[b].cut : a.plan[b].items; };
+  auto key = [&](int b) __attribute__((always_inline)) { return a.plan[b].items; };
   if (at >= key(a.B)) return false;
   int lo = 0;  // the last sequence whose count begins at or before `at` is in [lo, lo + 64 step)
 #pragma unroll
@@ -314,60 +324,94 @@ __device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, uint32_t
   f.b = __builtin_amdgcn_readfirstlane(lo);
   f.before = __builtin_amdgcn_readfirstlane(key(f.b));
   f.slots = __builtin_amdgcn_readfirstlane(a.plan[f.b].slots);
+  f.cut = __builtin_amdgcn_readfirstlane(a.plan[f.b].cut);
   f.whole = __builtin_amdgcn_readfirstlane(a.plan[f.b].whole);
-  f.L = __builtin_amdgcn_readfirstlane((int)a.plan[a.B].whole);
+  const int L = __builtin_amdgcn_readfirstlane((int)a.plan[a.B].whole);
   const Size s = size_of(a, f.b, g);
   f.size.qbase = __builtin_amdgcn_readfirstlane(s.qbase);
   f.size.nq = __builtin_amdgcn_readfirstlane(s.nq);
   f.size.nk = __builtin_amdgcn_readfirstlane(s.nk);
   f.size.tiles = __builtin_amdgcn_readfirstlane(s.tiles);
+  cut(a, f.size, g, L, f.C, f.chunk);
+  f.C = __builtin_amdgcn_readfirstlane(f.C);
+  f.chunk = __builtin_amdgcn_readfirstlane(f.chunk);
   return true;
 }
 
-// Item `at` (kCut: cut unit `at`, as its first chunk); false if there is none, or its
-// rows see no key of it.
-template <bool kCut>
+// Item `at`; false if there is none, or its rows see no key of it. kRecord: the item's
+// record number, and the first item's wave leaves the number of the records.
+template <bool kRecord>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item& it) {
-  const int g = a.H / a.Hkv;
+  const int g = a.g;
   Found f;
-  if (!(a.B <= 64 ? find_by_scan<1, kCut>(a, g, at, f)
-                  : a.B <= kPagedScan ? find_by_scan<kPagedScan / 64, kCut>(a, g, at, f)
-                                      : find_in_plan<kCut>(a, g, at, f)))
-    return false;
+  uint32_t n_cut = 0;
+  bool found;
+  if (a.B <= kPagedScan) {
+    found = a.B <= 64 ? find_by_scan<1, kRecord>(a, g, at, f, n_cut)
+                      : find_by_scan<kPagedScan / 64, kRecord>(a, g, at, f, n_cut);
+    if (kRecord && at == 0 && threadIdx.x == 0 && a.units) *a.units = n_cut;
+  } else {
+    found = find_in_plan(a, g, at, f);  // (the plan's launch has left the number)
+  }
+  if (!found) return false;
   it.b = f.b;
   it.qbase = f.size.qbase;
   it.nq = f.size.nq;
   it.nk = f.size.nk;
   it.few = is_few(a, it.nq, g);
-  int C;
-  cut(a, f.size, g, f.L, C, it.chunk);
+  int C = f.C;
+  it.chunk = f.chunk;
   uint32_t u = at - f.before;
   it.c = 0;
   it.slot = 0;
-  if (kCut) {
-    it.slot = (int)(f.slots + u * C);
-    u += f.whole;
-  } else if (C > 1 && u >= f.whole) {
+  it.record = -1;
+  if (C > 1 && u >= f.whole) {
     // all units' first chunks, then their second: neighbours read the same keys
     const uint32_t v = u - f.whole, n = (uint32_t)f.size.tiles * a.Hkv - f.whole;
     it.c = (int)(v / n);
     const uint32_t back = v - it.c * n;
     it.slot = (int)(f.slots + back * C);
+    if (kRecord) it.record = (int)(f.cut + back);
     u = f.whole + back;
   } else {
     C = 1;
     it.chunk = it.nk;
   }
-  it.kvh = (int)(u / (uint32_t)f.size.tiles);
+  it.kvh = f.size.tiles == 1 ? (int)u : (int)(u / (uint32_t)f.size.tiles);
   it.tile = f.size.tiles - 1 - (int)(u - (uint32_t)it.kvh * f.size.tiles);
   const int r0 = it.tile * tile_rows(it.few);
   it.rows = min(tile_rows(it.few), it.nq * g - r0);
   it.vis_end = row_limit(a, it, (r0 + it.rows - 1) / g, it.nk);
   it.n_chunks = C > 1 ? max(1, (int)(((uint32_t)it.vis_end + it.chunk - 1) / (uint32_t)it.chunk)) : 1;
   // (all of it is the wave's, but the divisions leave it in vector registers)
-  for (int* const p : {&it.kvh, &it.tile, &it.chunk, &it.c, &it.n_chunks, &it.slot, &it.rows, &it.vis_end})
+  for (int* const p : {&it.kvh, &it.tile, &it.chunk, &it.c, &it.n_chunks, &it.slot, &it.record, &it.rows, &it.vis_end})
     *p = __builtin_amdgcn_readfirstlane(*p);
   return it.c < it.n_chunks;
+}
+
+// What the launch that adds chunks up needs of a cut unit, written by its first chunk's
+// workgroup: planning it once more took that launch 2 us of 5.
+__device__ __forceinline__ u32x4_t* record_at(const PagedArgs& a, int n) {
+  return reinterpret_cast<u32x4_t*>(a.units) + kPagedRecord / 16 * (n + 1);  // (behind their number)
+}
+__device__ __forceinline__ void write_record(const PagedArgs& a, const Item& it) {
+  u32x4_t* const r = record_at(a, it.record);
+  r[0] = u32x4_t{(uint32_t)it.qbase, (uint32_t)it.nq, (uint32_t)it.nk, (uint32_t)it.kvh};
+  r[1] = u32x4_t{(uint32_t)it.tile, (uint32_t)it.slot, (uint32_t)it.n_chunks, (uint32_t)it.rows << 1 | (it.few ? 1 : 0)};
+}
+__device__ __forceinline__ void read_record(const PagedArgs& a, int n, Item& it) {
+  const u32x4_t* const r = record_at(a, n);
+  const u32x4_t x = r[0], y = r[1];
+  it.qbase = __builtin_amdgcn_readfirstlane(x.x);
+  it.nq = __builtin_amdgcn_readfirstlane(x.y);
+  it.nk = __builtin_amdgcn_readfirstlane(x.z);
+  it.kvh = __builtin_amdgcn_readfirstlane(x.w);
+  it.tile = __builtin_amdgcn_readfirstlane(y.x);
+  it.slot = __builtin_amdgcn_readfirstlane(y.y);
+  it.n_chunks = __builtin_amdgcn_readfirstlane(y.z);
+  const uint32_t w = __builtin_amdgcn_readfirstlane(y.w);
+  it.rows = (int)(w >> 1);
+  it.few = w & 1;
 }
 
 // ------------------------------------------------------- softmax and results
@@ -578,7 +622,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = a.H / a.Hkv;
+  const int g = a.g;
   const int kvh = it.kvh;
   const int pl = a.page_log2, mask = (1 << pl) - 1;
   const float c2 = a.scale_log2 * (kF8 && a.ks ? a.ks[kvh] : 1.0f);
@@ -970,7 +1014,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = a.H / a.Hkv;
+  const int g = a.g;
   const float inv_g = 1.0f / (float)g;
   const int kvh = it.kvh;
   const int pl = a.page_log2, mask_p = (1 << pl) - 1;
