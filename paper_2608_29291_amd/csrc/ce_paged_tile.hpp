@@ -462,24 +462,34 @@ __device__ __forceinline__ float part_load(__amdgpu_buffer_rsrc_t rs, uint32_t a
   return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (int)at, 0, kSC1));
 }
 
-// This workgroup's stores are complete and it arrives at counter `i`: is it the last of
-// n? A counter holds the call's token above the arrivals. Any other content, whatever
-// the workspace held before, counts as none: the first to come puts the token there,
-// the last leaves zero (a captured call replays with the same token). One exchange at
-// most, then one addition: sixteen that exchanged until it went well took 8 us.
-// `said`: a word of LDS that nobody else uses meanwhile.
-__device__ __forceinline__ bool arrive_last(const PagedArgs& a, int i, int n, int* said) {
+// A counter of arrivals holds the call's token above their number. Any other content,
+// whatever the workspace held before, counts as none. The last to arrive leaves zero (a
+// captured call replays with the same token), so this exchange of zero for the token,
+// made long before the arrival, is all that most calls need; what it found instead
+// of zero (the token, or anything) is returned.
+__device__ __forceinline__ unsigned long long expect_arrivals(const PagedArgs& a, int i) {
+  unsigned long long was = 0;
+  if (threadIdx.x == 0)
+    __hip_atomic_compare_exchange_strong(a.arrived + i, &was, a.token << 16, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT);
+  return was;
+}
+
+// This workgroup's stores are complete and it arrives at counter `i`, where
+// expect_arrivals found `was`: is it the last of n? One addition, and where memory held
+// something else one exchange before it; sixteen that exchanged until it went well
+// took 8 us. `said`: a word of LDS that nobody else uses meanwhile.
+__device__ __forceinline__ bool arrive_last(const PagedArgs& a, int i, int n, unsigned long long was, int* said) {
   asm volatile("" ::: "memory");
   wait_vmcnt<0>();
   __syncthreads();
   if (threadIdx.x == 0) {
     unsigned long long* const p = a.arrived + i;
-    unsigned long long was = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool first = (was >> 16) != a.token &&
-                       __hip_atomic_compare_exchange_strong(p, &was, (a.token << 16) + 1, __ATOMIC_RELAXED,
-                                                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (!first) was = __hip_atomic_fetch_add(p, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool last = !first && (int)(was & 0xffff) == n - 1;
+    if (was != 0 && (was >> 16) != a.token)  // (if it fails, another has put the token there)
+      __hip_atomic_compare_exchange_strong(p, &was, a.token << 16, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_AGENT);
+    was = __hip_atomic_fetch_add(p, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool last = (int)(was & 0xffff) == n - 1;
     if (last) __hip_atomic_store(p, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     *said = last;
   }
@@ -742,6 +752,9 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     }
   };
 
+  unsigned long long was = 0;
+  if (kDecode && it.n_chunks > 1) was = expect_arrivals(a, it.slot + it.c / kMeet * kMeet);
+
   f32x16_t oacc[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
@@ -941,7 +954,9 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     n = (n + kMeet - 1) / kMeet;
     idx /= kMeet;
     if (size > 1) {
-      if (!arrive_last(a, level * kPagedPlaces + slot, size, reinterpret_cast<int*>(ml))) return;
+      const int at = level * kPagedPlaces + slot;
+      if (level > 0) was = expect_arrivals(a, at);
+      if (!arrive_last(a, at, size, was, reinterpret_cast<int*>(ml))) return;
       int slot_v = slot;
       asm volatile("" : "+v"(slot_v));  // (sixteen offsets in scalar registers are too many)
       for (int rb = 0; rb < rows; rb += 8) {
