@@ -66,7 +66,7 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 //     finer cut: 64 of 2100 to 16001 keys, 8 bits, 78 (half as many: 114).
 //
 // How the chunks meet: of single tokens, in the launch itself (a second one would
-// cost 5 us of 18); of many rows, by a second launch over the whole chip, since one
+// cost 4 us of 15); of many rows, by a second launch over the whole chip, since one
 // workgroup would read 64 KB a chunk.
 
 struct Size {
@@ -622,7 +622,7 @@ __device__ __forceinline__ uint32_t vt_off(int d, uint32_t u) {
 //     paged_tile; a tile's fragments are read into registers at once, and the next
 //     tile's DMA takes their place. (Fragments loaded straight from memory read a line
 //     of 128 bytes in four instructions, and the line is gone from the cache between
-//     them: one token over 65537 keys 36 us, by DMA 33.7, 4.0 TB/s with start and end.)
+//     them: one token over 65537 keys 36 us, by DMA 33, 4.1 TB/s with start and end.)
 //   * 8-bit: K straight to registers in operand order (a line in four loads as well,
 //     but half the bytes: 64 tokens over 2100 to 16001 keys 78 us, 4.95 TB/s), V through
 //     registers, converted, exactly, and stored transposed in LDS.
