@@ -773,7 +773,8 @@ class KVCache:
                   for name, x in (("k_scale", self.k_scale), ("v_scale", self.v_scale)))
         tp = _chk(table, "page_table", _I32)
         c = CEKVCache(table.shape[0], h, d, page, n, table.shape[1], code, ld, kp, vp, ks, vs, tp)
-        self.__dict__["_known"] = (c, _device(), [(t, p) for t, p in (
+        c.device = _device()
+        self.__dict__["_known"] = (c, c.device, [(t, p) for t, p in (
             (k, kp), (v, vp), (table, tp), (self.k_scale, ks), (self.v_scale, vs)) if t is not None])
         return c
 
@@ -801,16 +802,20 @@ def _chk_strided(x, name, dtype, strides, unit):
     return p
 
 
-def _rows3(x, name, d, heads=None):
+def _rows3(x, name, device, d, heads=None):
     """Rows [n, heads, d] bf16 of a packed batch, possibly a part of wider rows: pointer,
     rows, heads and the rows' stride in elements."""
     try:
         n, h, dx = x.shape
-        st = x.stride()
         p = x.data_ptr()
-        if (x.dtype is torch.bfloat16 and x.get_device() == _device() and dx == d and (heads is None or h == heads)
-                and st[1:] == (d, 1) and st[0] >= h * d and not (st[0] | p >> 1) & 7):
-            return p, n, h, st[0] if n > 1 else h * d
+        if x.dtype is torch.bfloat16 and x.get_device() == device and dx == d and (heads is None or h == heads):
+            if x.is_contiguous():
+                if not p & 15:
+                    return p, n, h, h * d
+            else:
+                st = x.stride()
+                if st[1:] == (d, 1) and st[0] >= h * d and not (st[0] | p >> 1) & 7:
+                    return p, n, h, st[0] if n > 1 else h * d
     except (AttributeError, TypeError, ValueError):
         pass
     if x is None or x.dim() != 3 or x.shape[2] != d or (heads is not None and x.shape[1] != heads):
@@ -819,11 +824,11 @@ def _rows3(x, name, d, heads=None):
     return _chk_strided(x, name, torch.bfloat16, (d, 1), 8), n, h, x.stride(0) if n > 1 else h * d
 
 
-def _vec(t, name, n, dtype=_I32):
+def _vec(t, name, device, n, dtype=_I32):
     """Pointer of a contiguous device vector of at least n entries (what fails here is
     looked at again, for the message)."""
     try:
-        if t.dtype is dtype and t.get_device() == _device() and t.numel() >= n and t.is_contiguous():
+        if t.dtype is dtype and t.get_device() == device and t.numel() >= n and t.is_contiguous():
             p = t.data_ptr()
             if not p & 15:
                 return p
@@ -839,31 +844,32 @@ def ce_kv_reserve(cache: KVCache, lens, new_offsets, free_pages, free_count, sta
     place). new_offsets None: no new rows (slots may be None). slots holds as many
     entries as rows can come; status: 4-byte integer tensor for the CE_DEV_* bits."""
     cc = cache.c()
-    B = cc.B
+    B, dev = cc.B, cc.device
     rows = 0 if slots is None else slots.numel()
     if new_offsets is None and rows:
         raise ValueError("slots without new_offsets")
     if status is not None and status.dtype not in (torch.int32, torch.uint32):
         raise ValueError("status must be a 4-byte integer tensor")
-    lp, cp = _vec(lens, "lens", B), _vec(free_count, "free_count", 1)
+    lp, cp = _vec(lens, "lens", dev, B), _vec(free_count, "free_count", dev, 1)
     _check(lib.ce_kv_reserve(
-        ctypes.byref(cc), lp, None if new_offsets is None else _vec(new_offsets, "new_offsets", B + 1), rows,
-        None if reset is None else _vec(reset, "reset", B, _U8), _vec(free_pages, "free_pages", cc.n_pages), cp,
-        lp if lens_out is None else _vec(lens_out, "lens_out", B),
-        cp if free_count_out is None else _vec(free_count_out, "free_count_out", 1), _vec(start, "start", B),
-        _vec(slots, "slots", rows) if rows else None,
-        None if status is None else _vec(status, "status", 1, status.dtype), _stream(stream)), "ce_kv_reserve")
+        ctypes.byref(cc), lp, None if new_offsets is None else _vec(new_offsets, "new_offsets", dev, B + 1), rows,
+        None if reset is None else _vec(reset, "reset", dev, B, _U8), _vec(free_pages, "free_pages", dev, cc.n_pages), cp,
+        lp if lens_out is None else _vec(lens_out, "lens_out", dev, B),
+        cp if free_count_out is None else _vec(free_count_out, "free_count_out", dev, 1), _vec(start, "start", dev, B),
+        _vec(slots, "slots", dev, rows) if rows else None,
+        None if status is None else _vec(status, "status", dev, 1, status.dtype), _stream(stream)), "ce_kv_reserve")
 
 
 def ce_kv_append(cache: KVCache, k_new, v_new, slots, stream=None):
     """k_new, v_new [rows, H_kv, 128] bf16 (rows may be spaced, as in a fused projection)
     into their slots (ce_kv_reserve; -1 is skipped)."""
     cc = cache.c()
-    kp, n, _, kld = _rows3(k_new, "k_new", cc.head_dim, cc.n_kv_heads)
-    vp, nv, _, vld = _rows3(v_new, "v_new", cc.head_dim, cc.n_kv_heads)
+    dev, d, h = cc.device, cc.head_dim, cc.n_kv_heads
+    kp, n, _, kld = _rows3(k_new, "k_new", dev, d, h)
+    vp, nv, _, vld = _rows3(v_new, "v_new", dev, d, h)
     if nv != n:
         raise ValueError("k_new and v_new must have the same rows")
-    _check(lib.ce_kv_append(ctypes.byref(cc), kp, kld, vp, vld, _vec(slots, "slots", n), n, _stream(stream)),
+    _check(lib.ce_kv_append(ctypes.byref(cc), kp, kld, vp, vld, _vec(slots, "slots", dev, n), n, _stream(stream)),
            "ce_kv_append")
 
 
@@ -884,11 +890,12 @@ def ce_paged_attention(cache: KVCache, q, o, q_offsets, lens, causal, scale, ws=
     each sequence, o [rows, H, 128]; q_offsets int32 [B+1], lens int32 [B]. Without
     a workspace (alloc_paged_workspace) scratch comes from torch's allocator."""
     cc = cache.c()
-    qp, n, h, ld = _rows3(q, "q", cc.head_dim)
-    at = CEPagedAttn(h, n, _vec(q_offsets, "q_offsets", cc.B + 1), _vec(lens, "lens", cc.B), 1 if causal else 0,
+    dev, d, B = cc.device, cc.head_dim, cc.B
+    qp, n, h, ld = _rows3(q, "q", dev, d)
+    at = CEPagedAttn(h, n, _vec(q_offsets, "q_offsets", dev, B + 1), _vec(lens, "lens", dev, B), 1 if causal else 0,
                      float(scale))
-    op, no, _, old = _rows3(o, "o", cc.head_dim, h)
-    if no < n or old != h * cc.head_dim:
+    op, no, _, old = _rows3(o, "o", dev, d, h)
+    if no < n or old != h * d:
         raise ValueError("o must be contiguous and have q's rows")
     if ws is None:
         need = int(lib.ce_paged_workspace_size(ctypes.byref(cc), ctypes.byref(at)))
