@@ -267,3 +267,59 @@ def test_refusals_of_the_binding():
         with pytest.raises((ValueError, ce.CERouterError)):
             ce.ce_kv_reserve(c, *args)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_rows_past_four_gib(dtype):
+    """Queries and outputs whose offsets need more than 32 bits, behind rows that see no token."""
+    import torch
+    import paper_2608_29291_amd as ce
+    H, Hkv, first = 64, 8, 270000
+    new, lens = [0, 40, 1], [0, 300, 777]
+    p = U.Paged(lens, Hkv, 16, dtype, seed=81)
+    c = p.cache()
+    n = first + sum(new)
+    q = torch.full((n, H, U.DH), 0.5, dtype=torch.bfloat16, device="cuda")
+    o = torch.full_like(q, 77.0)
+    x = rows(new, H)
+    q[first:] = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    ce.ce_paged_attention(c, q, o, i32([0, first, first + 40, n]), i32(lens), True, U.DH ** -0.5)
+    U.check(o[first:].float().cpu().numpy(), *p.answer(x, new, True, U.DH ** -0.5))
+    assert not o[:first:1000].any() and not o[first - 1].any()
+
+
+def test_most_sequences():
+    """The largest batch, one token each, all over the same few pages."""
+    import torch
+    import paper_2608_29291_amd as ce
+    B, H, Hkv = 65535, 6, 2
+    p = U.Paged([160], Hkv, 16, "bf16", seed=91)
+    lens = np.random.default_rng(2).integers(0, 161, B)
+    p.table = np.repeat(p.table, B, 0)
+    q = rows([B], H)
+    qd = torch.from_numpy(q).to(torch.bfloat16).cuda()
+    o = torch.full_like(qd, 77.0)
+    ce.ce_paged_attention(p.cache(), qd, o, torch.arange(B + 1, dtype=torch.int32, device="cuda"), i32(lens.tolist()), True,
+                          U.DH ** -0.5)
+    got = o.float().cpu().numpy()
+    assert not (got == 77.0).all((1, 2)).any()
+    k, v = p.k_used[0], p.v_used[0]
+    for b in (0, 1, 255, 256, 511, 4095, 4096, 40000, B - 1):
+        p.k_used, p.v_used = [k[:lens[b]]], [v[:lens[b]]]
+        U.check(got[b:b + 1], *p.answer(q[b:b + 1], [1], True, U.DH ** -0.5))
+
+
+def test_every_sequence_of_the_largest_batch_gets_a_page():
+    import torch
+    import paper_2608_29291_amd as ce
+    B = 65535
+    k = torch.empty(B + 5, 1, 16, U.DH, dtype=torch.bfloat16, device="cuda")
+    c = ce.KVCache(k, k, torch.full((B, 2), -1, dtype=torch.int32, device="cuda"))
+    lens, count, status = torch.zeros(B, dtype=torch.int32, device="cuda"), i32([B + 5]), i32([9])
+    start, slots = torch.full_like(lens, 9), torch.full_like(lens, 9)
+    free = torch.arange(B + 5, dtype=torch.int32, device="cuda")
+    ce.ce_kv_reserve(c, lens, torch.arange(B + 1, dtype=torch.int32, device="cuda"), free, count, start, slots, status=status)
+    page = torch.arange(B + 4, 4, -1, dtype=torch.int32, device="cuda")  # from the top of the stack
+    assert torch.equal(c.page_table[:, 0], page) and (c.page_table[:, 1] == -1).all()
+    assert torch.equal(slots, page * 16) and not start.any() and (lens == 1).all()
+    assert count.item() == 5 and status.item() == 0

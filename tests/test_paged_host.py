@@ -130,6 +130,13 @@ def test_workspace():
     assert size(cache(B=65535, n_kv_heads=65, page_stride=65 * 2048), attn(n_heads=65)) == 0  # refused
 
 
+def test_workspace_for_more_rows_serves_fewer():
+    for B in (4, 40, 300):
+        for heads in (2, 12, 64):
+            sizes = [size(cache(max_pages=1000, B=B), attn(n_heads=heads, q_capacity=n)) for n in range(1, 700, 7)]
+            assert sizes == sorted(sizes)
+
+
 def test_nothing_to_do_is_no_launch():
     assert append(cache(), rows=0, k=None, v=None, slots=None) == 0
     assert attend(cache(), attn(q_capacity=0), q=None, o=None, ws=None, ws_bytes=0) == 0
