@@ -946,7 +946,8 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   }
   if constexpr (!kDecode) return;
   // ---- the chunks meet, 16 at a time, eight rows at a time; all their loads are in
-  //      flight together ----
+  //      flight together (always sixteen, some of them twice, made 16 tokens over 551
+  //      to 3100 keys 14.4 us instead of 14.0) ----
   int n = it.n_chunks, idx = it.c, stride = 1;
   for (int level = 0; n > 1; ++level) {
     const int first = idx / kMeet * kMeet, size = min(kMeet, n - first);
@@ -959,12 +960,13 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
       if (!arrive_last(a, at, size, was, reinterpret_cast<int*>(ml))) return;
       int slot_v = slot;
       asm volatile("" : "+v"(slot_v));  // (sixteen offsets in scalar registers are too many)
-      for (int rb = 0; rb < rows; rb += 8) {
+      auto meet = [&](auto n_c, int rb) __attribute__((always_inline)) {
+        constexpr int kN = decltype(n_c)::value;
         const int r = min(rb + r_first, rows - 1);
-        f32x4_t y[kMeet];
-        float mc[kMeet], lc[kMeet];
+        f32x4_t y[kN];
+        float mc[kN], lc[kN];
 #pragma unroll
-        for (int i = 0; i < kMeet; ++i) {
+        for (int i = 0; i < kN; ++i) {
           const uint32_t at = (uint32_t)(slot_v + min(i, size - 1) * stride) * kSlotBytes<kDecode>;
           y[i] = part_load4(prs, at + r * (kDh * 4) + qd * 16);
           mc[i] = part_load(prs, at + kStats<kDecode> + r * 4);
@@ -973,9 +975,9 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
         f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
         float m = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kMeet; ++i) m = fmaxf(m, mc[i]);
+        for (int i = 0; i < kN; ++i) m = fmaxf(m, mc[i]);
 #pragma unroll
-        for (int i = 0; i < kMeet; ++i)
+        for (int i = 0; i < kN; ++i)
           if (i < size) {
             const float wi = weight(mc[i], m, c2);
             l = fmaf(lc[i], wi, l);
@@ -988,7 +990,14 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
           else
             finish(r, x, l);
         }
-      }
+      };
+      for (int rb = 0; rb < rows; rb += 8)
+        if (size <= kMeet / 4)
+          meet(std::integral_constant<int, kMeet / 4>{}, rb);
+        else if (size <= kMeet / 2)
+          meet(std::integral_constant<int, kMeet / 2>{}, rb);
+        else
+          meet(std::integral_constant<int, kMeet>{}, rb);
     }
     stride *= kMeet;
   }
