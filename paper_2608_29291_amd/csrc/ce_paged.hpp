@@ -56,7 +56,7 @@ struct PagedArgs {
   unsigned long long* arrived;  // single tokens: counters of the chunks that meet, kPagedPlaces a level
   uint32_t* units;   // else the number of cut units and a record of each, or NULL: none is cut
   unsigned long long token;     // of this call, 48 bits
-  PagedPlan* plan;   // B > kPagedScan: the sequences, then the items and (whole) the chunk length
+  PagedPlan* plan;   // B > kPagedScan: the sequences, then the items, (whole) the chunk length and (slots) if half of the places are filled
 };
 
 constexpr int kPagedScan = 256;    // sequences that a wave plans by itself (four a lane)

@@ -135,15 +135,18 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
     if (b < a.B) a.plan[b].whole = wh;
     base += total;
   }
+  const float w_all = w;
+  const uint32_t all = (uint32_t)min(base, (int64_t)1 << 30);
   if (whole) w = sum(rest);
   int L = chunk_length(w);
   for (;;) {
+    const bool half = a.decode && half_places(a, L, all, w_all, most);
     int64_t items = 0, slots = 0, cuts = 0;
     auto put = [](int64_t x) { return (uint32_t)min(x, (int64_t)1 << 30); };
     for (int b0 = 0; b0 < a.B; b0 += 512) {
       const int b = b0 + tid;
       Counts c = {0, 0, 0};
-      if (b < a.B) c = counts_of(a, size_of(a, b, g), g, L, a.plan[b].whole);
+      if (b < a.B) c = counts_of(a, size_of(a, b, g), g, L, half, a.plan[b].whole);
       const int64_t i0 = items + scan(c.items, total);
       items += total;
       const int64_t s0 = slots + scan(c.slots, total);
@@ -158,6 +161,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
     }
     if (tid == 0) {
       a.plan[a.B].items = put(items);
+      a.plan[a.B].slots = half;
       a.plan[a.B].whole = (uint32_t)L;
       if (a.units) *a.units = put(cuts);
     }

@@ -24,8 +24,10 @@ constexpr int kGroup = 4;          // MFMA operands read from LDS together, one 
 constexpr float kLazy = 8.0f;      // headroom of the running maximum (exponent of 2)
 constexpr int kMinFew = 128;       // least keys of a chunk: one tile of 32 for each wave
 constexpr int kWholeFew = 640;     // least keys of a sequence that is cut for a few rows
-constexpr int kMaxHalf = 1024;     // keys per place up to which single tokens fill half of the places
+constexpr int kMaxHalf = 512;      // keys per place up to which single tokens fill half of the places,
+constexpr int kMaxEven = 1024;     // and where the sequences are about equal
 constexpr int kMaxMeet = 512;      // keys per chunk up to which no more than kMeet meet
+constexpr int kMostOver = 24;      // chunks that are made kMeet whatever their keys
 constexpr int kMinTile = 256;
 constexpr int kMeet = 16;          // chunks that meet at a time in the launch itself
 constexpr int kOLd = kDh + 4;      // floats per row of paged_few's outputs in LDS
@@ -59,11 +61,16 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 // not pay (us, single tokens at 28 / 4 heads, bf16, before / after):
 //   * below 640 keys not at all: 1 x 300 keys 9.7 / 7.5, 32 x 600 14.9 / 11.1;
 //   * into at most 16 chunks, that meet at once, as long as these have no more than 512
-//     keys: 1 x 4000 13.0 / 10.6, 8 x 5 drafted tokens over 333 to 4103 18.3 / 15.9;
-//   * single tokens into half as many where a place's share is at most 1024 keys: one
+//     keys: 1 x 4000 13.0 / 10.6, 8 x 5 drafted tokens over 333 to 4103 18.3 / 15.9; of
+//     17 to 24 chunks 16 are made in any case: 15 sequences up to 13516 29.4 / 24.5,
+//     29 up to 16281, 12 / 2 heads, 24.6 / 21.7 (of up to 32: 34 up to 16222, 8 bits,
+//     8 / 1 heads, 15.8 / 17.0);
+//   * single tokens into half as many where a place's share is at most 512 keys: one
 //     workgroup a CU keeps the memory as busy, and fewer chunks meet: 16 sequences of
-//     551 to 3100 16.4 / 15.3, 32 x 1000 18.2 / 14.8. Above, unequal sequences need the
-//     finer cut: 64 of 2100 to 16001 keys, 8 bits, 78 (half as many: 114).
+//     551 to 3100 16.4 / 15.3, 32 x 1000 18.2 / 14.8. Up to 1024 so where the sequences
+//     are about equal (1 x 65537 34.5 / 32.9, 39 of one length, 4 / 4 heads, 53 / 50);
+//     unequal ones need the finer cut there (half as many / this: 57, 31, 43 and 48
+//     drawn sequences 38 / 29, 56 / 46, 40 / 27, 68 / 51).
 //
 // How the chunks meet: of single tokens, in the launch itself (a second one would
 // cost 4 us of 15); of many rows, by a second launch over the whole chip, since one
@@ -102,13 +109,18 @@ __device__ __forceinline__ int chunk_length(float w) {
   return l > 1e9f ? 1 << 30 : (int)l + 1;
 }
 
+// May single tokens fill half of the places? (units units, w keys, the dearest `most`)
+__device__ __forceinline__ bool half_places(const PagedArgs& a, int L, uint32_t units, float w, float most) {
+  return L <= kMaxHalf / 2 || (L <= kMaxEven / 2 && most * (float)units <= 1.25f * w);
+}
+
 // A sequence's chunks (a whole number of its waves' tiles).
-__device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, int& C, int& chunk) {
+__device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, bool half, int& C, int& chunk) {
   const bool few = is_few(a, s.nq, g);
   if (few) {
     const int l = 2 * min(L, 1 << 29);  // (2^30: nothing is cut)
-    C = s.nk < kWholeFew ? 1 : s.nk / max(a.decode && l <= kMaxHalf ? 2 * l : l, kMinFew);
-    if (C > kMeet && s.nk <= kMeet * kMaxMeet) C = kMeet;
+    C = s.nk < kWholeFew ? 1 : s.nk / max(half ? 2 * l : l, kMinFew);
+    if (C > kMeet && (s.nk <= kMeet * kMaxMeet || C <= kMostOver)) C = kMeet;
   } else {
     C = s.nk / max(L, kMinTile);
   }
@@ -140,9 +152,9 @@ struct Counts {
   uint32_t items, slots, cut;
   int C, chunk;
 };
-__device__ __forceinline__ Counts counts_of(const PagedArgs& a, const Size& s, int g, int L, uint32_t whole) {
+__device__ __forceinline__ Counts counts_of(const PagedArgs& a, const Size& s, int g, int L, bool half, uint32_t whole) {
   Counts c;
-  cut(a, s, g, L, c.C, c.chunk);
+  cut(a, s, g, L, half, c.C, c.chunk);
   const uint32_t n = (uint32_t)s.tiles * a.Hkv;
   c.cut = c.C > 1 ? n - whole : 0;
   c.slots = c.cut * c.C;
@@ -236,7 +248,9 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
   const uint32_t units_to = wave_scan(units);
   w = wave_sum(w);
   const uint32_t all = __builtin_amdgcn_readlane(units_to, 63);
-  const uint32_t whole = whole_units(all, w, wave_max(most));
+  most = wave_max(most);
+  const float w_all = w;
+  const uint32_t whole = whole_units(all, w, most);
   if (whole) {  // what the rest costs
     float rest = 0.0f;
     uint32_t first = units_to - units;
@@ -253,11 +267,12 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
   uint32_t wh[kPer], sum, sum_s, sum_c, to, slots_to;
   for (;;) {
     uint32_t first = units_to - units;
+    const bool half = !kRecord && half_places(a, L, all, w_all, most);  // (a call of single tokens has no records)
     sum = sum_s = sum_c = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       wh[i] = whole_of(a, s[i], first, whole);
-      n[i] = counts_of(a, s[i], g, L, wh[i]);
+      n[i] = counts_of(a, s[i], g, L, half, wh[i]);
       first += (uint32_t)s[i].tiles * a.Hkv;
       sum += n[i].items;
       sum_s += n[i].slots;
@@ -327,12 +342,13 @@ __device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, uint32_t
   f.cut = __builtin_amdgcn_readfirstlane(a.plan[f.b].cut);
   f.whole = __builtin_amdgcn_readfirstlane(a.plan[f.b].whole);
   const int L = __builtin_amdgcn_readfirstlane((int)a.plan[a.B].whole);
+  const bool half = __builtin_amdgcn_readfirstlane(a.plan[a.B].slots) != 0;
   const Size s = size_of(a, f.b, g);
   f.size.qbase = __builtin_amdgcn_readfirstlane(s.qbase);
   f.size.nq = __builtin_amdgcn_readfirstlane(s.nq);
   f.size.nk = __builtin_amdgcn_readfirstlane(s.nk);
   f.size.tiles = __builtin_amdgcn_readfirstlane(s.tiles);
-  cut(a, f.size, g, L, f.C, f.chunk);
+  cut(a, f.size, g, L, half, f.C, f.chunk);
   f.C = __builtin_amdgcn_readfirstlane(f.C);
   f.chunk = __builtin_amdgcn_readfirstlane(f.chunk);
   return true;
