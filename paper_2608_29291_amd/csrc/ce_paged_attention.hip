@@ -173,8 +173,9 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
 
 // Partial results of the cut units, in chunk order. Bound: latency, 3 us
 // for 8 x 5 rows and 6 for 512 queries over 8704 keys, whose 30 MB come from the
-// caches. Workgroup (unit, z): 32 rows z of
-// a 128-row tile, as wave z of its chunks' workgroups left them; of a few rows, eight.
+// caches. Workgroup (unit, y): the 32 rows y % 4 of a 128-row tile, as that wave of
+// its chunks' workgroups left them (of 16 parts, a quarter of their values); of a few
+// rows, eight.
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
   Item it;
   read_record(a, blockIdx.x, it);  // (any content behind the last, and not used)
@@ -240,9 +241,20 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
       add(One{}, std::integral_constant<int, 16>{}, slot + at, 0, r, [&](int) { return d; });
     }
   } else {
-    for (int z = blockIdx.y; 32 * z < it.rows; z += gridDim.y)  // accumulators 4 wave .. +3
-      add(Four{}, Four{}, slot + ((z * 16 + 4 * wave) * 64 + lane) * 4, 256, 32 * z + (lane & 31),
+    const int z = blockIdx.y & 3, r = 32 * z + (lane & 31);
+    if (32 * z >= it.rows) return;
+    if (gridDim.y == 4) {  // accumulators 4 wave .. +3
+      add(Four{}, Four{}, slot + ((z * 16 + 4 * wave) * 64 + lane) * 4, 256, r,
           [&](int v) { return 32 * wave + 8 * v + 4 * (lane >> 5); });
+    } else {
+      const int acc = (int)(blockIdx.y & ~3u) + wave;
+      const float* const p = slot + ((z * 16 + acc) * 64 + lane) * 4;
+      auto dims = [&](int) { return 8 * acc + 4 * (lane >> 5); };
+      if (n <= 4)
+        add(One{}, Four{}, p, 0, r, dims);
+      else
+        add(One{}, std::integral_constant<int, 16>{}, p, 0, r, dims);
+    }
   }
 }
 
@@ -315,7 +327,12 @@ hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
     hipLaunchKernelGGL(paged_attention_kernel<false>, blocks, threads, 0, stream, a, group);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.cut_units == 0) return e;
-  hipLaunchKernelGGL(paged_combine_kernel, dim3(p.cut_units, 4), threads, 0, stream, a);
+  // Few units have many chunks: four times as many workgroups read sixteen of them at
+  // a time (8 / 1 heads, five sequences of 6 to 9 tokens over 111 to 11538 keys 23.9,
+  // 19.4 us; 40 of 2 to 9, 12 / 2 heads, up to 11349, 29.3, 25.7). With more units that
+  // costs what it gains (two chunks of 701 beside 30 tokens 36.0, 37.2).
+  const int parts = p.cut_units <= 128 ? 16 : 4;
+  hipLaunchKernelGGL(paged_combine_kernel, dim3(p.cut_units, parts), threads, 0, stream, a);
   return hipGetLastError();
 }
 
