@@ -33,7 +33,8 @@ enum { CE_E4M3 = 2 };
 enum {
   CE_DEV_NO_PAGES = 4,  /* the free pages did not suffice for every sequence           */
   CE_DEV_TOO_LONG = 8,  /* a sequence would outgrow its row of the page table          */
-  CE_DEV_BAD_CACHE = 16 /* a length, count or page number out of its range was clamped */
+  CE_DEV_BAD_CACHE = 16 /* a length or count out of its range was clamped, or a page number out of
+                         * its range was given back or handed out (as it is: its rows get no slot) */
 };
 
 /*

@@ -139,7 +139,9 @@ __global__ __launch_bounds__(1024) void kv_reserve_kernel(ReserveArgs a) {
       __syncthreads();
       for (int i = tid; i < pushed; i += 1024) {
         const int k = last_at_most(first, 1024, i);
-        a.free_pages[count + i] = a.table[(int64_t)(s0 + k) * a.max_pages + (i - first[k])];
+        const int page = a.table[(int64_t)(s0 + k) * a.max_pages + (i - first[k])];
+        if ((uint32_t)page >= (uint32_t)a.n_pages) st |= CE_DEV_BAD_CACHE;  // (and again where it is popped)
+        a.free_pages[count + i] = page;
       }
       count += pushed;
       __syncthreads();
