@@ -1,5 +1,6 @@
 """State that outlives a call of the paged cache: page numbers that go back on the free
-stack."""
+stack, and a handle whose tensors change in place."""
+import numpy as np
 import pytest
 
 import paged_util as U
@@ -41,3 +42,33 @@ def test_page_numbers_out_of_range_are_reported_when_they_go_back(bad, B):
     reset[0] = 1
     ce.ce_kv_reserve(c, lens, None, free, count, start, None, reset=reset, status=status)
     assert status.item() == 0 and free[:4].tolist() == [7, 6, 5, 4]
+
+
+def attend(c, p, q, lens):
+    import torch
+    import paper_2608_29291_amd as ce
+    qd = torch.from_numpy(q).to(torch.bfloat16).cuda()
+    o = torch.empty_like(qd)
+    ce.ce_paged_attention(c, qd, o, torch.arange(len(q) + 1, dtype=torch.int32, device="cuda"), i32(lens), True, U.DH ** -0.5)
+    return o.float().cpu().numpy()
+
+
+def test_a_table_that_changes_in_place_is_seen():
+    """Same memory, other rows: the next call takes the table as it is now."""
+    p = U.Paged([40, 33, 50, 20], 2, 16, "bf16", seed=5, extra_cols=0)
+    q = U.bf16(np.random.default_rng(1).standard_normal((4, 4, U.DH)))
+    c = p.cache()
+    U.check(attend(c, p, q, p.lens), *p.answer(q, [1] * 4, True, U.DH ** -0.5))
+    c.page_table.resize_(2, 4)
+    assert c.c().B == 2 and c.c().max_pages == 4
+    c.page_table.resize_(4, 4)
+    U.check(attend(c, p, q, p.lens), *p.answer(q, [1] * 4, True, U.DH ** -0.5))
+    c.page_table.t_()
+    with pytest.raises(ValueError, match="page_table"):
+        attend(c, p, q, p.lens)
+    c.page_table.t_()
+    c.k.resize_(p.n_pages - 1, 2, 16, U.DH)
+    with pytest.raises(ValueError, match="one shape"):
+        attend(c, p, q, p.lens)
+    c.v.resize_(p.n_pages - 1, 2, 16, U.DH)
+    assert c.c().n_pages == p.n_pages - 1
