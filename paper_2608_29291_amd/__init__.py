@@ -756,6 +756,10 @@ class KVCache:
                 return known[0]
         return self._check()
 
+    def __getstate__(self):
+        """The tensors: what c() remembers holds pointers into this process's memory."""
+        return {n: x for n, x in self.__dict__.items() if n != "_known"}
+
     def _check(self) -> CEKVCache:
         k, v, table = self.k, self.v, self.page_table
         if k is None or v is None or k.dim() != 4 or v.shape != k.shape:

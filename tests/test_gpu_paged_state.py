@@ -1,5 +1,8 @@
 """State that outlives a call of the paged cache: page numbers that go back on the free
-stack, and a handle whose tensors change in place."""
+stack, and a handle whose tensors change in place, is copied or pickled after its first call."""
+import copy
+import pickle
+
 import numpy as np
 import pytest
 
@@ -72,3 +75,19 @@ def test_a_table_that_changes_in_place_is_seen():
         attend(c, p, q, p.lens)
     c.v.resize_(p.n_pages - 1, 2, 16, U.DH)
     assert c.c().n_pages == p.n_pages - 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_a_used_cache_is_copied_and_pickled(dtype):
+    p = U.Paged([700, 33], 2, 16, dtype, seed=6)
+    q = U.bf16(np.random.default_rng(1).standard_normal((2, 4, U.DH)))
+    c = p.cache()
+    want = attend(c, p, q, p.lens)
+    others = [copy.copy(c), copy.deepcopy(c)]
+    if dtype == "bf16":  # (pickle.loads fails on any float8 tensor: torch's own limit)
+        others.append(pickle.loads(pickle.dumps(c)))
+    for other in others:
+        assert np.array_equal(attend(other, p, q, p.lens), want)
+    deep = copy.deepcopy(c)
+    deep.v.zero_()  # pages of its own
+    assert not attend(deep, p, q, p.lens).any() and np.array_equal(attend(c, p, q, p.lens), want)

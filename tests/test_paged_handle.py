@@ -1,5 +1,8 @@
 """KVCache on the CPU, with the checks that need device memory put aside: what it remembers
 of its tensors after the first call."""
+import copy
+import pickle
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -46,3 +49,13 @@ def test_a_change_of_type_is_seen(cache):
     for x in (cache.k, cache.v):
         x.data = x.view(torch.float8_e4m3fn)[..., :128].as_strided(x.shape, [2 * s for s in x.stride()[:-1]] + [1])
     assert cache.c().dtype == ce.CE_E4M3
+
+
+def test_a_used_handle_is_copied_and_pickled(cache):
+    cache.c()
+    for other in (copy.copy(cache), copy.deepcopy(cache), pickle.loads(pickle.dumps(cache))):
+        assert other.k_scale is None and torch.equal(other.page_table, cache.page_table)
+        assert other.k.stride() == cache.k.stride() and other.c().k == other.k.data_ptr()
+        other.page_table.resize_(2, 4)
+        assert other.c().B == 2 and (cache.c().B == 6 or other.page_table is cache.page_table)
+        other.page_table.resize_(6, 4)
