@@ -22,6 +22,7 @@ constexpr int kBK = 32;            // keys per block: one pass of the softmax
 constexpr int kKBytes = kKT * kRowB;
 constexpr int kGroup = 4;          // MFMA operands read from LDS together, one group ahead
 constexpr float kLazy = 8.0f;      // headroom of the running maximum (exponent of 2)
+constexpr float kFar = 8192.0f;    // size of a maximum's exponent from which differences are taken first
 constexpr int kMinFew = 128;       // least keys of a chunk: one tile of 32 for each wave
 constexpr int kWholeFew = 640;     // least keys of a sequence that is cut for a few rows
 constexpr int kMaxHalf = 512;      // keys per place up to which single tokens fill half of the places,
@@ -439,6 +440,25 @@ __device__ __forceinline__ float weight(float m, float m_all, float c2) {
   return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - m_all) * c2);
 }
 
+// The exponent of a weight is fma(score, c2, -mc) with mc = m c2 rounded. That rounding,
+// 2^-25 of mc, is common to the keys of one maximum, but not to those of another that meet
+// them (2^-12 at kFar), and past 2^31 it is hundreds and more: 2 to that is no float. From
+// kFar on, rows take (score - m) c2, exact up to two roundings of the difference itself;
+// scores so large are rare, and a wave looks for them where its maxima move. The branch costs
+// the tiles 0.2 to 0.7% (a look at every block 1 to 2.2%; kept in the branch that moves the
+// maxima, which such rows then always take, 0.6 to 1.5%).
+__device__ __forceinline__ float exponent_of(float m, float c2) { return m == -__builtin_inff() ? 0.0f : m * c2; }
+__device__ __forceinline__ bool any_far(float mc) { return __builtin_amdgcn_ballot_w64(fabsf(mc) > kFar) != 0; }
+// Scores become exponents, each row's by its own rule, whatever the wave's other rows do, and
+// the scale and offset still to come those of nothing.
+__device__ __forceinline__ void far_scores(f32x16_t& sc, float m, float c2, float& mc, float& ce) {
+  const bool far = fabsf(mc) > kFar;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) sc[v] = far ? (sc[v] - m) * c2 : fmaf(sc[v], c2, -mc);
+  mc = 0.0f;
+  ce = 1.0f;
+}
+
 // Factor of the output: scale of the values / sum; a row that sees no key is zero,
 // one that sees only scores of -infinity is 0 / 0.
 __device__ __forceinline__ float normalizer(float l, float vs, bool sees) {
@@ -555,7 +575,7 @@ __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, c
   int lhalf = (threadIdx.x >> 5) & 1;
   asm volatile("" : "+v"(lhalf));  // no address of this path is formed before it
   const int mask = (1 << a.page_log2) - 1;
-  const float mc = m == -__builtin_inff() ? 0.0f : m * c2;
+  const float mc = exponent_of(m, c2);
 #pragma unroll
   for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
   for (; k0 < vis1; k0 += kstep)
@@ -585,7 +605,7 @@ __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, c
         __builtin_amdgcn_sched_barrier(0);  // (few registers are left)
       }
       sc += __shfl_xor(sc, 32);
-      const float p = __builtin_amdgcn_exp2f(fmaf(sc, c2, -mc));
+      const float p = __builtin_amdgcn_exp2f(fabsf(mc) > kFar ? (sc - m) * c2 : fmaf(sc, c2, -mc));
       if (j < vis) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {  // dims 8 v + 4 lhalf .. +3
@@ -775,6 +795,8 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
 #pragma unroll
   for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
   float m_run = -__builtin_inff(), l_run = 0.0f;
+  float mc_run = 0.0f;  // exponent of m_run
+  bool far = false;     // that of some row is far
 
   const int step = 4 * kBK;
   int k0 = kbeg + wave * kBK;
@@ -842,12 +864,15 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
       for (int i = 0; i < 4; ++i) oacc[i] *= alpha;
       l_run *= alpha;
       m_run = m_new;
+      mc_run = exponent_of(m_run, c2);
+      far = any_far(mc_run);
     }
-    const float mc = m_run == -__builtin_inff() ? 0.0f : m_run * c2;
+    float mc = mc_run, ce = c2;
+    if (far) far_scores(sc, m_run, c2, mc, ce);
     float rs = 0.0f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], c2, -mc));
+      sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], ce, -mc));
       rs += sc[v];
     }
     l_run += rs + __shfl_xor(rs, 32);
@@ -1168,6 +1193,8 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
 #pragma unroll
   for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
   float m_run = -__builtin_inff(), l_run = 0.0f;  // l_run: this lane's keys only until the epilogue
+  float mc_run = 0.0f;  // exponent of m_run
+  bool far = false;     // that of some row is far
   const int qi = q0 + small_div(h0 + min(32 * wave + lrow, it.rows - 1), inv_g);  // this lane's query
   const int vis = row_limit(a, it, qi, kend);  // keys [0, vis) are seen
   const int vis0 = row_limit(a, it, __builtin_amdgcn_readfirstlane(qi), kend);  // by the wave's first row
@@ -1235,18 +1262,21 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
       if (m_new != -__builtin_inff()) alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c2);
       l_run *= alpha;
       m_run = m_new;
+      mc_run = exponent_of(m_run, c2);
+      far = any_far(mc_run);
     }
-    const float mc = m_run == -__builtin_inff() ? 0.0f : m_run * c2;
+    float mc = mc_run, ce = c2;
+    if (far) far_scores(sc, m_run, c2, mc, ce);
     // Step k: exponential k, the exponent of k + 1, and the pair before k is added
     // and packed; nothing in a step waits for the step's own exponential.
-    float rs = 0.0f, p[16], ex = fmaf(sc[0], c2, -mc);
+    float rs = 0.0f, p[16], ex = fmaf(sc[0], ce, -mc);
     auto soft = [&](int k) __attribute__((always_inline)) {
       if (k < 16) {
         p[k] = __builtin_amdgcn_exp2f(ex);
         asm volatile("" : "+v"(p[k]));  // this and the others keep the values between their fences
       }
       if (k < 15) {
-        ex = fmaf(sc[k + 1], c2, -mc);
+        ex = fmaf(sc[k + 1], ce, -mc);
         asm volatile("" : "+v"(ex));
       }
       if (k >= 2 && !(k & 1)) {

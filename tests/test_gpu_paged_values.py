@@ -1,5 +1,5 @@
 """Values at the ends of their range in attention over the paged cache: infinite scores beside
-finite rows."""
+finite rows, scores so large that one key has all the weight."""
 import numpy as np
 import pytest
 
@@ -43,3 +43,33 @@ def test_infinite_scores_touch_the_rows_that_see_them(new, lens):
     for r in range(sum(new)):
         assert bad[r].tolist() == [(h == 1 and r == 0) or (h >= 6 and new[0] // 2 <= r < new[0]) for h in range(12)]
     U.check(go(p, q, new), want, top)
+
+
+def by_far(p, q, new, least=2.0 ** -12):
+    """Rows and heads whose highest score is ahead of all others by `least` of its size: far more
+    than a fp32 sum of 128 products errs by (about 2^-16 of it)."""
+    at, sure = 0, np.zeros(q.shape[:2], bool)
+    g = q.shape[1] // p.hkv
+    for b, n in enumerate(new):
+        for i in range(n):
+            for h in range(q.shape[1]):
+                s = np.sort(np.float64(p.k_used[b][:p.lens[b] - n + i + 1, h // g]) @ np.float64(q[at + i, h]))
+                sure[at + i, h] = len(s) < 2 or s[-1] - s[-2] > least * np.abs(s).max()
+        at += n
+    return sure
+
+
+@pytest.mark.parametrize("new,lens", SHAPES)
+@pytest.mark.parametrize("size,scale", [(2e3, 0.1), (3e4, 0.1), (1e6, 0.1), (1e9, 0.1), (1e18, 100.0)])
+def test_scores_of_any_size(size, scale, new, lens):
+    """From 1e6 to past float32's range: the output is the highest key's value."""
+    rng = np.random.default_rng(25)
+    k = [U.bf16(rng.standard_normal((n, 2, U.DH)) * size) for n in lens]
+    p = U.Paged(lens, 2, 16, "bf16", seed=25, k=k)
+    q = U.bf16(rows(sum(new), 12) * size)
+    want, top = p.answer(q, new, True, float(np.float32(scale)))
+    sure = by_far(p, q, new)
+    assert sure.mean() > 0.98
+    got = go(p, q, new, scale)
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want)[sure] <= U.TOL * top[sure][:, None]).all()
