@@ -564,18 +564,20 @@ __device__ __forceinline__ int64_t page_at(const PagedArgs& a, int kvh, int page
   return (int64_t)((uint64_t)(uint32_t)(ok ? page : 0) * a.page_bytes) + ((uint32_t)kvh << a.page_log2) * kPageRow<kF8>;
 }
 
-// Output of a wave's 32 rows again, key by key (the scores' maximum m and sum are
-// right as they are): keys k0 + n kstep + 0 .. 31 below vis1, a lane's row sees those
-// below vis. qf: the row, 8 dims a chunk, chunk s from dim 8 (2 s + lane / 32), or with
-// kWide from 16 (2 (s / 2) + lane / 32) + 8 (s % 2). Slow, and reached only where a
-// value is NaN or infinite in a sequence's last rows.
+// Output of a wave's 32 rows again, key by key, with maxima and sums of its own: the scores
+// that it forms differ from those of the matrix instructions in their rounding, which at a score
+// of 1e6 is a tenth and more of the exponent. Keys k0 + n kstep + 0 .. 31 below vis1, a
+// lane's row sees those below vis. qf: the row, 8 dims a chunk, chunk s from dim
+// 8 (2 s + lane / 32), or with kWide from 16 (2 (s / 2) + lane / 32) + 8 (s % 2). Slow, and
+// reached only where a value is NaN or infinite in a sequence's last rows.
 template <bool kF8, bool kWide>
 __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, const u32x4_t (&qf)[8], f32x16_t (&oacc)[4],
-                                        float m, float c2, int vis, int k0, int kstep, int vis1) {
+                                        float& m, float& l, float c2, int vis, int k0, int kstep, int vis1) {
   int lhalf = (threadIdx.x >> 5) & 1;
   asm volatile("" : "+v"(lhalf));  // no address of this path is formed before it
   const int mask = (1 << a.page_log2) - 1;
-  const float mc = exponent_of(m, c2);
+  m = -__builtin_inff();
+  l = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
   for (; k0 < vis1; k0 += kstep)
@@ -583,7 +585,6 @@ __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, c
       bool ok;
       const int page = __builtin_amdgcn_readfirstlane(a.table[(int64_t)b * a.max_pages + (j >> a.page_log2)]);
       const int64_t at = page_at<kF8>(a, kvh, page, ok) + (int64_t)(j & mask) * kPageRow<kF8>;
-      if (!ok) continue;  // zeros
       const char* const kp = a.k + at + lhalf * (kF8 && !kWide ? 8 : 16);
       const char* const vp = a.v + at + lhalf * (kF8 ? 4 : 8);
       auto lo = [](uint32_t x) __attribute__((always_inline)) { return __uint_as_float(x << 16); };
@@ -591,13 +592,13 @@ __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, c
       float sc = 0.0f;
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        u32x4_t x;  // the 8 values that meet chunk s of the row
+        u32x4_t x = {0, 0, 0, 0};  // the 8 values that meet chunk s of the row
         if constexpr (kF8) {
-          const u32x2_t y =
-              *reinterpret_cast<const u32x2_t*>(kp + (kWide ? (s >> 1) * 32 + (s & 1) * 8 : s * 16));
+          u32x2_t y = {0, 0};
+          if (ok) y = *reinterpret_cast<const u32x2_t*>(kp + (kWide ? (s >> 1) * 32 + (s & 1) * 8 : s * 16));
           const u32x2_t e = e4m3_to_bf16(y.x), f = e4m3_to_bf16(y.y);
           x = u32x4_t{e.x, e.y, f.x, f.y};
-        } else {
+        } else if (ok) {
           x = *reinterpret_cast<const u32x4_t*>(kp + s * 32);
         }
 #pragma unroll
@@ -605,8 +606,18 @@ __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, c
         __builtin_amdgcn_sched_barrier(0);  // (few registers are left)
       }
       sc += __shfl_xor(sc, 32);
-      const float p = __builtin_amdgcn_exp2f(fabsf(mc) > kFar ? (sc - m) * c2 : fmaf(sc, c2, -mc));
       if (j < vis) {
+        const float m_new = fmaxf(m, sc);
+        if (m_new > m) {
+          const float al = weight(m, m_new, c2);
+          l *= al;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) oacc[i] *= al;
+          m = m_new;
+        }
+        const float p = __builtin_amdgcn_exp2f((m == -__builtin_inff() ? sc : sc - m) * c2);
+        l += p;
+        if (!ok) continue;  // (values of zero)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {  // dims 8 v + 4 lhalf .. +3
           u32x2_t x;
@@ -927,7 +938,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     }
   }
   if (vis0 < vis1 && any_nan(oacc))
-    paged_redo<kF8, kF8>(a, it.b, kvh, qf, oacc, m_run, c2, vis, kbeg + wave * kBK, step, vis1);
+    paged_redo<kF8, kF8>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg + wave * kBK, step, vis1);
 
   // ---- the four waves meet: common maximum, scaled outputs through LDS ----
   int tid_e = threadIdx.x;
@@ -1431,8 +1442,10 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
 #pragma unroll
     for (int j = 8; j < 16; ++j) mfma_step<true>(oacc[j & 3], frag(j, 0, 1), pb[(j - 8) >> 2]);
     const int last_key = min(kend, kbeg + ntiles * kKT);
-    if (a.causal && vis0 < last_key && any_nan(oacc))
-      paged_redo<kF8, false>(a, it.b, kvh, qf, oacc, m_run, c2, vis, kbeg, kBK, last_key);
+    if (a.causal && vis0 < last_key && any_nan(oacc)) {
+      paged_redo<kF8, false>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg, kBK, last_key);
+      if (lhalf) l_run = 0.0f;  // (the whole sum, once)
+    }
   }
 
   l_run += __shfl_xor(l_run, 32);

@@ -73,3 +73,34 @@ def test_scores_of_any_size(size, scale, new, lens):
     got = go(p, q, new, scale)
     assert np.isfinite(got).all()
     assert (np.abs(got - want)[sure] <= U.TOL * top[sure][:, None]).all()
+
+
+@pytest.mark.parametrize("new,lens", SHAPES[1:])
+def test_unseen_values_beside_large_scores(new, lens):
+    """A NaN value behind a row's mask: that output is formed again, by the same exponents."""
+    rng = np.random.default_rng(26)
+    k = [U.bf16(rng.standard_normal((n, 2, U.DH)) * 1e6) for n in lens]
+    v = [U.bf16(rng.standard_normal((n, 2, U.DH))) for n in lens]
+    v[0][-1, :, 5] = np.nan
+    p = U.Paged(lens, 2, 16, "bf16", seed=26, k=k, v=v)
+    q = U.bf16(rows(sum(new), 12) * 1e6)
+    want, top = p.answer(q, new, True, float(np.float32(0.1)))
+    sure = by_far(p, q, new)
+    assert sure.mean() > 0.98 and np.isnan(want[new[0] - 1, :, 5]).all() and np.isnan(want).sum() == 12
+    got = go(p, q, new, 0.1)
+    U.check(got[sure][:, None], want[sure][:, None], top[sure][:, None])
+
+
+@pytest.mark.parametrize("new,lens", SHAPES[1:])
+def test_unseen_values_beside_a_page_that_is_none(new, lens):
+    """An output that is formed again counts the keys of a missing page, all zeros, as well."""
+    v = [U.bf16(np.random.default_rng(27).standard_normal((n, 2, U.DH))) for n in lens]
+    v[0][-1, :, 5] = np.nan
+    for dtype in ("bf16", "e4m3"):
+        p = U.Paged(lens, 2, 16, dtype, seed=27, v=v)
+        for b, col in ((0, 3), (0, 40), (1, 0)):
+            p.table[b, col] = -1
+            for x in (p.k_used[b], p.v_used[b]):
+                x[16 * col:16 * col + 16] = 0.0
+        q = rows(sum(new), 12)
+        U.check(go(p, q, new), *p.answer(q, new, True, U.DH ** -0.5))
