@@ -148,9 +148,10 @@ typedef struct ce_paged_attn {
  *       aligned, contents on entry do not matter. Calls that may overlap, captured
  *       ones among them, need workspaces of their own
  * Lengths are clamped to [0, max_pages * page_size]; a page number outside
- * [0, n_pages) reads as zeros. fp32 scores, statistics and accumulation (scale * Q K^T
- * may be past float32, Q K^T may not); the probabilities are rounded to bf16 for the
- * product with V. Deterministic.
+ * [0, n_pages) reads as zeros. fp32 scores, statistics and accumulation (scale * k_scale
+ * and scale * Q K^T may be past float32 or round to zero, the products of Q with stored
+ * keys may not be past it); the probabilities are rounded to bf16 for the product with V.
+ * Deterministic.
  * Errors: CE_ERR_INVALID_ARG for null pointers, sizes, a scale that is not
  * positive with scale * log2 e finite or causal outside {0, 1}; CE_ERR_UNSUPPORTED outside
  * the limits, for more than 4096 query heads a key/value head, q_capacity * n_heads

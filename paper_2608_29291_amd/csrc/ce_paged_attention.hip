@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = a.g;
   const int n = it.n_chunks;
-  const float c2 = a.scale_log2 * (a.ks ? a.ks[it.kvh] : 1.0f);
+  const float c2 = score_scale(a, it.kvh);
   const float vs = a.vs ? a.vs[it.kvh] : 1.0f;
   constexpr int kPart = kSlotBytes<false> / 4;
   const float* const slot = a.part + (int64_t)it.slot * kPart;

@@ -433,6 +433,19 @@ __device__ __forceinline__ void read_record(const PagedArgs& a, int n, Item& it)
 
 // ------------------------------------------------------- softmax and results
 
+// Scale of raw scores in the exponent: softmax scale times log2 e, times that of 8-bit keys
+// (ks). Both may be any positive float, their product may be none: 0 would make NaN of a masked
+// score (-inf 0), and infinity one of a score of zero. The least and the largest float
+// stand in for them: under the first, raw scores, below 2^128, weigh alike to within 2^-20;
+// under the second, raw scores that differ at all (by 1e-36 and more, where they are normal
+// floats) differ by more than the exponent holds, as they do under the product.
+// (bf16: the host has seen to it, and the value stays a scalar.)
+__device__ __forceinline__ float score_scale(const PagedArgs& a, int kvh) {
+  if (!a.ks) return a.scale_log2;
+  const float c = a.scale_log2 * a.ks[kvh];
+  return c < 0x1p-149f ? 0x1p-149f : (c > 0x1.fffffep127f ? 0x1.fffffep127f : c);
+}
+
 // Weight of a partial result with maximum m under the maximum m_all (raw scores;
 // c2: their scale times log2 e). Without any finite maximum it counts nothing,
 // except that NaN times 0 stays NaN.
@@ -682,7 +695,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   const int g = a.g;
   const int kvh = it.kvh;
   const int pl = a.page_log2, mask = (1 << pl) - 1;
-  const float c2 = a.scale_log2 * (kF8 && a.ks ? a.ks[kvh] : 1.0f);
+  const float c2 = kF8 ? score_scale(a, kvh) : a.scale_log2;
   const int kbeg = it.c * it.chunk;
   const int kend = min(it.nk, kbeg + it.chunk);
   const int rows = it.rows;
@@ -1094,7 +1107,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   const float inv_g = 1.0f / (float)g;
   const int kvh = it.kvh;
   const int pl = a.page_log2, mask_p = (1 << pl) - 1;
-  const float c2 = a.scale_log2 * (kF8 && a.ks ? a.ks[kvh] : 1.0f);
+  const float c2 = kF8 ? score_scale(a, kvh) : a.scale_log2;
   const int kbeg = it.c * it.chunk;
   const int kend = min(it.nk, kbeg + it.chunk);
   const int ntiles = max(0, min(kend, it.vis_end) - kbeg + kKT - 1) / kKT;

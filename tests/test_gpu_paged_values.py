@@ -1,5 +1,6 @@
 """Values at the ends of their range in attention over the paged cache: infinite scores beside
-finite rows, scores so large that one key has all the weight."""
+finite rows, scores so large that one key has all the weight,
+softmax scales times key scales that leave float32."""
 import numpy as np
 import pytest
 
@@ -104,3 +105,44 @@ def test_unseen_values_beside_a_page_that_is_none(new, lens):
                 x[16 * col:16 * col + 16] = 0.0
         q = rows(sum(new), 12)
         U.check(go(p, q, new), *p.answer(q, new, True, U.DH ** -0.5))
+
+
+def quantized(lens, ks, vs, seed=22):
+    """8-bit pages of standard normal values under given scales."""
+    p = U.Paged(lens, 2, 16, "e4m3", seed=seed, scales=False)
+    p.ks, p.vs = np.full(2, ks, np.float32), np.full(2, vs, np.float32)
+    p.k_used = [x * np.float64(p.ks[0]) for x in p.k_used]
+    p.v_used = [x * np.float64(p.vs[0]) for x in p.v_used]
+    return p
+
+
+@pytest.mark.parametrize("new,lens", SHAPES)
+@pytest.mark.parametrize("scale,ks", [(1e-10, 1e-36), (1e-30, 1e-30), (1e-44, 0.02), (1e-3, 1e-40)])
+def test_scores_near_zero(scale, ks, new, lens):
+    """softmax scale times key scale rounds to zero or next to it: every key that is seen has
+    the same weight, to within 2^-20."""
+    p = quantized(lens, ks, 1.0)
+    q = rows(sum(new), 12)
+    U.check(go(p, q, new, scale), *p.answer(q, new, True, float(np.float32(scale))))
+
+
+def test_a_denormal_softmax_scale():
+    p = U.Paged([900, 40], 2, 16, "bf16", seed=23)
+    for new in ([1, 1], [3, 2], [80, 40]):
+        q = rows(sum(new), 12)
+        U.check(go(p, q, new, 1e-44), *p.answer(q, new, True, float(np.float32(1e-44))))
+
+
+@pytest.mark.parametrize("new,lens", SHAPES)
+def test_a_score_scale_past_float32(new, lens):
+    """The two scales multiply to 1e40 and the queries are that small: the scores are ordinary
+    float32 numbers (near 1e11), so far apart that the highest takes all the weight."""
+    p = quantized(lens, 1e10, 1.0)
+    q = U.bf16(rows(sum(new), 12) * 1e-30)
+    want, top = p.answer(q, new, True, float(np.float32(1e30)))
+    sure = by_far(p, q, new)
+    assert sure.mean() > 0.99
+    got = go(p, q, new, 1e30)
+    assert np.isfinite(got).all()
+    err = np.abs(got - want)[sure]
+    assert (err <= U.TOL * top[sure][:, None]).all()
