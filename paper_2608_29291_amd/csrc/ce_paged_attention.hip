@@ -227,10 +227,11 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
     if (r >= it.rows) return;
     const int row = it.tile * tile_rows(it.few) + r;
     const int qi = row / g;
-    const float inv = normalizer(l, vs, row_limit(a, it, qi, it.nk) > 0);
+    const float inv = normalizer(l, row_limit(a, it, qi, it.nk) > 0);
     char* const o = a.o + ((int64_t)(it.qbase + qi) * a.H + it.kvh * g + (row - qi * g)) * kRowB;
 #pragma unroll
-    for (int v = 0; v < kN; ++v) store4<true>(o + 2 * out(v), x[v][0] * inv, x[v][1] * inv, x[v][2] * inv, x[v][3] * inv);
+    for (int v = 0; v < kN; ++v)
+      store4<true>(o + 2 * out(v), x[v][0] * inv * vs, x[v][1] * inv * vs, x[v][2] * inv * vs, x[v][3] * inv * vs);
   };
   using One = std::integral_constant<int, 1>;
   using Four = std::integral_constant<int, 4>;

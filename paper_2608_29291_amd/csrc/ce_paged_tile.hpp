@@ -472,10 +472,11 @@ __device__ __forceinline__ void far_scores(f32x16_t& sc, float m, float c2, floa
   ce = 1.0f;
 }
 
-// Factor of the output: scale of the values / sum; a row that sees no key is zero,
-// one that sees only scores of -infinity is 0 / 0.
-__device__ __forceinline__ float normalizer(float l, float vs, bool sees) {
-  return sees ? vs / l : 0.0f;
+// Outputs are sum * normalizer * scale of the values, in this order: scale / l could be a
+// float of a few bits (a scale of 1e-38 and 600000 keys). A row that sees no key is zero, one
+// that sees only scores of -infinity is 0 / 0.
+__device__ __forceinline__ float normalizer(float l, bool sees) {
+  return sees ? 1.0f / l : 0.0f;
 }
 
 // Partial results of the chunks of a unit meet through the workspace, in chunk order,
@@ -982,9 +983,9 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   const __amdgpu_buffer_rsrc_t prs = part_rsrc<kDecode>(a);
   auto finish = [&](int r, const f32x4_t& x, float l) __attribute__((always_inline)) {
     const int q2 = small_div(h0 + r, 1.0f / (float)g);
-    const float inv = normalizer(l, vs, row_limit(a, it, q0 + q2, it.nk) > 0);
-    store4<true>(a.o + ((int64_t)(it.qbase + q0 + q2) * a.H + kvh * g + (h0 + r - q2 * g)) * kRowB + 8 * qd, x[0] * inv,
-                 x[1] * inv, x[2] * inv, x[3] * inv);
+    const float inv = normalizer(l, row_limit(a, it, q0 + q2, it.nk) > 0);
+    store4<true>(a.o + ((int64_t)(it.qbase + q0 + q2) * a.H + kvh * g + (h0 + r - q2 * g)) * kRowB + 8 * qd, x[0] * inv * vs,
+                 x[1] * inv * vs, x[2] * inv * vs, x[3] * inv * vs);
   };
   auto keep = [&](int slot, int r, const f32x4_t& x, float m, float l) __attribute__((always_inline)) {
     const uint32_t at = (uint32_t)slot * kSlotBytes<kDecode>;
@@ -1479,14 +1480,15 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   // ---- O = O^T / l, turned through LDS into whole rows (256 bytes by 16 lanes).
   //      The wave uses its own 8 KB of the K buffers, which no wave reads after
   //      the last barrier. ----
-  const float inv = normalizer(l_run, kF8 && a.vs ? a.vs[kvh] : 1.0f, row_limit(a, it, qi, it.nk) > 0);
+  const float inv = normalizer(l_run, row_limit(a, it, qi, it.nk) > 0);
+  const float vs = kF8 && a.vs ? a.vs[kvh] : 1.0f;
   char* const ob = kbuf + wave * 32 * kRowB;
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
     for (int g4 = 0; g4 < 4; ++g4)
-      store4<true>(ob + lrow * kRowB + (((4 * db + g4) ^ (lrow & 15)) << 4) + 8 * lhalf, oacc[db][4 * g4] * inv,
-                   oacc[db][4 * g4 + 1] * inv, oacc[db][4 * g4 + 2] * inv, oacc[db][4 * g4 + 3] * inv);
+      store4<true>(ob + lrow * kRowB + (((4 * db + g4) ^ (lrow & 15)) << 4) + 8 * lhalf, oacc[db][4 * g4] * inv * vs,
+                   oacc[db][4 * g4 + 1] * inv * vs, oacc[db][4 * g4 + 2] * inv * vs, oacc[db][4 * g4 + 3] * inv * vs);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
   for (int i = 0; i < 8; ++i) {

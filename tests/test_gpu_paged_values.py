@@ -1,6 +1,6 @@
 """Values at the ends of their range in attention over the paged cache: infinite scores beside
 finite rows, scores so large that one key has all the weight,
-softmax scales times key scales that leave float32."""
+softmax scales times key scales that leave float32, value scales next to zero."""
 import numpy as np
 import pytest
 
@@ -146,3 +146,19 @@ def test_a_score_scale_past_float32(new, lens):
     assert np.isfinite(got).all()
     err = np.abs(got - want)[sure]
     assert (err <= U.TOL * top[sure][:, None]).all()
+
+
+@pytest.mark.parametrize("vs", [1.25e-38, 1e-36, 1e30])
+def test_value_scales_far_from_one(vs):
+    """Many keys of one weight: the quotient vs / (sum of weights) would be a float32 with a few
+    bits left, the output is an ordinary one."""
+    keys, times = 4096, 150
+    p = U.Paged([keys], 1, 256, "e4m3", seed=24, scales=False, v=[np.full((keys, 1, U.DH), 448.0)])
+    n = keys // 256
+    p.table = np.tile(p.table[:, :n], (1, times))
+    p.lens = [keys * times]
+    p.ks, p.vs = np.ones(1, np.float32), np.full(1, vs, np.float32)
+    want = 448.0 * np.float64(p.vs[0])
+    for new in ([1], [2], [40]):
+        got = go(p, np.zeros((sum(new), 2, U.DH), np.float32), new)
+        assert (np.abs(got - want) <= U.TOL * want).all(), (new, got.min(), got.max(), want)
