@@ -36,6 +36,7 @@
 #include "ce_host.hpp"
 #include "ce_paged.hpp"
 #include "ce_paged_tile.hpp"
+#include "ce_paged_token.hpp"
 
 namespace ce {
 
@@ -261,18 +262,6 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
 
 }  // namespace
 
-// A token that no earlier call of the process had and that memory is unlikely to
-// hold by chance: a counter through a mix of its bits (a bijection), 48 bits of it, not 0.
-static uint64_t paged_token() {
-  static std::atomic<uint64_t> calls{0};
-  uint64_t x = (calls.fetch_add(1, std::memory_order_relaxed) + 1) * 0x9e3779b97f4a7c15ull;
-  x ^= x >> 31;
-  x *= 0xd6e8feb86659fd93ull;
-  x ^= x >> 32;
-  x &= (1ull << 48) - 1;
-  return x ? x : 1;
-}
-
 PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
   PagedGrid p = {};
   if (q_cap <= 0) return p;
@@ -308,7 +297,8 @@ hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
   const int64_t grid = (p.items + unit - 1) / unit * unit;
   a.grid = (uint32_t)grid;
   a.decode = p.decode;
-  a.token = paged_token();
+  static std::atomic<uint64_t> calls{0};
+  a.token = paged_token(calls.fetch_add(1, std::memory_order_relaxed) + 1);
   if (a.B > kPagedScan) {
     hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(512), 0, stream, a);
     const hipError_t e = hipGetLastError();

@@ -513,10 +513,11 @@ __device__ __forceinline__ float part_load(__amdgpu_buffer_rsrc_t rs, uint32_t a
 }
 
 // A counter of arrivals holds the call's token above their number. Any other content,
-// whatever the workspace held before, counts as none. The last to arrive leaves zero (a
-// captured call replays with the same token), so this exchange of zero for the token,
-// made long before the arrival, is all that most calls need; what it found instead
-// of zero (the token, or anything) is returned.
+// whatever the workspace held before, counts as none. The last to arrive leaves zero, and a
+// group of one, where nobody arrives, the token with no arrivals: so a captured call may
+// replay with the same token. This exchange of zero for the token, made long before the
+// arrival, is all that most calls need; what it found instead of zero (the token, or
+// anything) is returned.
 __device__ __forceinline__ unsigned long long expect_arrivals(const PagedArgs& a, int i) {
   unsigned long long was = 0;
   if (threadIdx.x == 0)
