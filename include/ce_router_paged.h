@@ -158,7 +158,7 @@ typedef struct ce_paged_attn {
  * >= 2^28 or B * n_kv_heads >= 2^22;
  * CE_ERR_WORKSPACE; CE_ERR_HIP.
  * ce_paged_workspace_size depends on the sizes in cache and attn only (no device
- * pointer is read), is at most 35 MB, and 0 where none is used or the call
+ * pointer is read), is at most 35135744 bytes, and 0 where none is used or the call
  * would refuse the sizes.
  */
 size_t ce_paged_workspace_size(const ce_kv_cache* cache, const ce_paged_attn* attn);
