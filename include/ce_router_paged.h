@@ -82,7 +82,9 @@ typedef struct ce_kv_cache {
  *     pages and these and those that the sequences before it needed (refused
  *     for want of pages or not) are more than the stack holds;
  *   - row r of sequence b becomes token start[b] + r - new_offsets[b], in slot
- *     page * page_size + row of the page.
+ *     page * page_size + row of the page. Rows of a refused sequence (start -1) are not
+ *     in the cache: ce_kv_append skips them, and what ce_paged_attention gives for
+ *     them is attention over the end of what the cache holds, not their answer.
  *   cache       k and v are not touched (and may be NULL); n_kv_heads, head_dim,
  *               dtype, page_stride are not read
  *   lens        device int32 [B]

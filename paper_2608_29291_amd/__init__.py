@@ -892,7 +892,8 @@ def alloc_paged_workspace(cache: KVCache, q_rows: int, n_heads: int):
 def ce_paged_attention(cache: KVCache, q, o, q_offsets, lens, causal, scale, ws=None, stream=None):
     """q [rows, H, 128] bf16 (rows may be spaced) over the cache's first lens[b] tokens of
     each sequence, o [rows, H, 128]; q_offsets int32 [B+1], lens int32 [B]. Without
-    a workspace (alloc_paged_workspace) scratch comes from torch's allocator."""
+    a workspace (alloc_paged_workspace) scratch comes from torch's allocator, so a program
+    that captures without torch.cuda.graph passes one of its own."""
     cc = cache.c()
     dev, d, B = cc.device, cc.head_dim, cc.B
     qp, n, h, ld = _rows3(q, "q", dev, d)
