@@ -1097,8 +1097,8 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
 //     after each MFMA of two products that do not depend on it: the scores of the
 //     next block and the output of the block before.
 // Bound: MFMA and the softmax's VALU about alike (four chunks of 2048 queries over 7000
-// to 10240 keys, 28 heads, causal: 875 us, 1.09 PFLOP/s, MFMA busy 66% of the time
-// and VALU 60%; 4 x 2176 queries over 2304 keys, 12 heads: 133 us, 0.93). 64 rows a
+// to 10240 keys, 28 heads, causal: 887 us, 1.07 PFLOP/s, MFMA busy 65% of the time
+// and VALU 60%; 4 x 2176 queries over 2304 keys, 12 heads: 134 us, 0.92). 64 rows a
 // wave, with half the LDS reads, leave one wave a SIMD: 986 and 161.
 template <bool kF8>
 __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem, const Item& it) {
