@@ -226,6 +226,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
   for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
   float m_run = -__builtin_inff(), l_run = 0.0f;
+  float mc_run = 0.0f;  // exponent of m_run
+  bool far = false;     // that of some row is far
 
   const int step = 4 * kKT;
   int k0 = kbeg + wave * kKT;
@@ -261,12 +263,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (int i = 0; i < 4; ++i) oacc[i] *= alpha;
       l_run *= alpha;
       m_run = m_new;
+      mc_run = exponent_of(m_run, a.scale_log2);
+      far = any_far(mc_run);
     }
-    const float mc = m_run == -__builtin_inff() ? 0.0f : m_run * a.scale_log2;
+    float mc = mc_run, ce = a.scale_log2;
+    if (far) far_scores(sc, m_run, a.scale_log2, mc, ce);
     float rs = 0.0f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2, -mc));
+      sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], ce, -mc));
       rs += sc[v];
     }
     l_run += rs + __shfl_xor(rs, 32);

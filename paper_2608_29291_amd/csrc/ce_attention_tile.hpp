@@ -47,6 +47,7 @@
 #include <type_traits>
 
 #include "ce_device.hpp"
+#include "ce_softmax.hpp"
 
 namespace ce {
 
@@ -186,6 +187,8 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, char* const sm
 #pragma unroll
   for (int i = 0; i < 4; ++i) oacc[i] = f32x16_t{};
   float m_run = -__builtin_inff(), l_run = 0.0f;  // l_run: this lane's keys only until the epilogue
+  float mc_run = 0.0f;  // exponent of m_run
+  bool far = false;     // that of some row is far
   const int vis = a.causal ? min(nk, qi + off + 1) : nk;              // keys [0, vis) are visible
   const int vis0 = a.causal ? min(nk, q0 + 32 * wave + off + 1) : nk;  // the wave's smallest
 
@@ -249,11 +252,14 @@ __device__ __forceinline__ void attention_tile(const AttnArgs& a, char* const sm
       if (m_new != -__builtin_inff()) alpha = __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2);
       l_run *= alpha;
       m_run = m_new;
+      mc_run = exponent_of(m_run, a.scale_log2);
+      far = any_far(mc_run);
     }
-    const float mc = m_run == -__builtin_inff() ? 0.0f : m_run * a.scale_log2;
+    float mc = mc_run, ce = a.scale_log2;
+    if (far) far_scores(sc, m_run, a.scale_log2, mc, ce);
     float rs = 0.0f, even = 0.0f;
     auto prob = [&](int e) __attribute__((always_inline)) {
-      float p = __builtin_amdgcn_exp2f(fmaf(sc[e], a.scale_log2, -mc));
+      float p = __builtin_amdgcn_exp2f(fmaf(sc[e], ce, -mc));
       asm volatile("" : "+v"(p));  // this and the next keep the value between its fences
       if (e & 1) {
         rs += even + p;

@@ -6,6 +6,7 @@
 
 #include "ce_device.hpp"
 #include "ce_paged.hpp"
+#include "ce_softmax.hpp"
 
 namespace ce {
 
@@ -22,7 +23,6 @@ constexpr int kBK = 32;            // keys per block: one pass of the softmax
 constexpr int kKBytes = kKT * kRowB;
 constexpr int kGroup = 4;          // MFMA operands read from LDS together, one group ahead
 constexpr float kLazy = 8.0f;      // headroom of the running maximum (exponent of 2)
-constexpr float kFar = 8192.0f;    // size of a maximum's exponent from which differences are taken first
 constexpr int kMinFew = 128;       // least keys of a chunk: one tile of 32 for each wave
 constexpr int kWholeFew = 640;     // least keys of a sequence that is cut for a few rows
 constexpr int kMaxHalf = 512;      // keys per place up to which single tokens fill half of the places,
@@ -451,25 +451,6 @@ __device__ __forceinline__ float score_scale(const PagedArgs& a, int kvh) {
 // except that NaN times 0 stays NaN.
 __device__ __forceinline__ float weight(float m, float m_all, float c2) {
   return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - m_all) * c2);
-}
-
-// The exponent of a weight is fma(score, c2, -mc) with mc = m c2 rounded. That rounding,
-// 2^-25 of mc, is common to the keys of one maximum, but not to those of another that meet
-// them (2^-12 at kFar), and past 2^31 it is hundreds and more: 2 to that is no float. From
-// kFar on, rows take (score - m) c2, exact up to two roundings of the difference itself;
-// scores so large are rare, and a wave looks for them where its maxima move. The branch costs
-// the tiles 0.2 to 0.7% (a look at every block 1 to 2.2%; kept in the branch that moves the
-// maxima, which such rows then always take, 0.6 to 1.5%).
-__device__ __forceinline__ float exponent_of(float m, float c2) { return m == -__builtin_inff() ? 0.0f : m * c2; }
-__device__ __forceinline__ bool any_far(float mc) { return __builtin_amdgcn_ballot_w64(fabsf(mc) > kFar) != 0; }
-// Scores become exponents, each row's by its own rule, whatever the wave's other rows do, and
-// the scale and offset still to come those of nothing.
-__device__ __forceinline__ void far_scores(f32x16_t& sc, float m, float c2, float& mc, float& ce) {
-  const bool far = fabsf(mc) > kFar;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) sc[v] = far ? (sc[v] - m) * c2 : fmaf(sc[v], c2, -mc);
-  mc = 0.0f;
-  ce = 1.0f;
 }
 
 // Outputs are sum * normalizer * scale of the values, in this order: scale / l could be a
