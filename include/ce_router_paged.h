@@ -76,8 +76,8 @@ typedef struct ce_kv_cache {
  * new_offsets[b + 1] - new_offsets[b] more (ce_topk_compact's kept_offsets).
  *   - pages given back are pushed on the free stack, sequences in order, each
  *     sequence's pages in table order (users of a page are not counted: one that
- *     stands in two rows of the table, which ce_paged_attention may read, is pushed
- *     by each, and its caller gives it back once);
+ *     stands in two rows of the table, which ce_paged_attention may read, would be
+ *     pushed by each of them, so only one of the two may be handed on);
  *   - then every sequence in order pops the pages it still needs from the top
  *     into its row of the table. A sequence is refused, and stays as it is
  *     (after its reset), if its row of the table is too short, or if it needs
