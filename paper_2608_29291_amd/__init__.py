@@ -25,6 +25,12 @@ built.
                            the compressed cache in pages (bf16 or e4m3): pages and slots for a step's
                            new rows, made on the device; their keys and values into them; attention
                            of the new rows over the cache
+    ce_draft_masks, ce_paged_tree_attention, ce_verify_drafts, ce_kv_keep, ce_kv_trim
+                           drafted decoding over that cache (include/ce_router_draft.h): masks and
+                           positions of trees, attention under masks of bits, the rows that the
+                           target's probabilities accept, and what stays of the others' pages
+    ce_rotary              rotary positions of packed rows, in one axis or several
+                           (include/ce_router_rotary.h)
 """
 from __future__ import annotations
 
@@ -43,6 +49,8 @@ CE_DEV_BAD_OFFSETS, CE_DEV_OVERFLOW = 1, 2
 CE_WS_TOPK, CE_WS_FFN, CE_WS_BLOCK, CE_WS_BLOCK_GAP, CE_WS_FFN_PRUNED, CE_WS_SCORE = 0, 1, 2, 3, 4, 5
 CE_E4M3 = 2
 CE_DEV_NO_PAGES, CE_DEV_TOO_LONG, CE_DEV_BAD_CACHE = 4, 8, 16
+CE_DEV_BAD_TREE, CE_DEV_TOO_WIDE = 32, 64
+CE_ROTARY_HALVES, CE_ROTARY_PAIRS = 0, 1
 
 EXPORTED = [
     "ce_status_string", "ce_version", "ce_num_keep", "ce_kept_count_host", "ce_workspace_size",
@@ -109,6 +117,16 @@ class CEPagedAttn(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class CEDrafts(ctypes.Structure):
+    _fields_ = [("B", _i32), ("row_capacity", _i32), ("offsets", _p), ("parents", _p), ("tokens", _p)]
+
+
+class CERotaryDesc(ctypes.Structure):
+    _fields_ = [("rows", _i32), ("n_heads", _i32), ("head_dim", _i32), ("n_pairs", _i32), ("n_axes", _i32),
+                ("layout", _i32), ("inverse", _i32), ("dtype", _i32), ("n_positions", _i32), ("freq", _p), ("axis", _p),
+                ("positions", _p), ("index", _p)]
+
+
 def _sig(name, res, args):
     f = getattr(lib, name)
     f.restype = res
@@ -157,6 +175,15 @@ _sig("ce_kv_append", ctypes.c_int, [ctypes.POINTER(CEKVCache), _p, ctypes.c_int6
 _sig("ce_paged_workspace_size", ctypes.c_size_t, [ctypes.POINTER(CEKVCache), ctypes.POINTER(CEPagedAttn)])
 _sig("ce_paged_attention", ctypes.c_int, [ctypes.POINTER(CEKVCache), ctypes.POINTER(CEPagedAttn), _p, ctypes.c_int64,
                                           _p, _p, ctypes.c_size_t, _p])
+_sig("ce_paged_tree_attention", ctypes.c_int, [ctypes.POINTER(CEKVCache), ctypes.POINTER(CEPagedAttn), _p, _i32, _p,
+                                               ctypes.c_int64, _p, _p, ctypes.c_size_t, _p])
+_sig("ce_draft_masks", ctypes.c_int, [ctypes.POINTER(CEDrafts), _i32, _p, _p, _p, _p, _p])
+_sig("ce_verify_workspace_size", ctypes.c_size_t, [ctypes.POINTER(CEDrafts), _i32, ctypes.c_int])
+_sig("ce_verify_drafts", ctypes.c_int, [ctypes.POINTER(CEDrafts), _i32, _p, ctypes.c_int64, ctypes.c_int, _p, _p,
+                                        ctypes.c_int64, _p, _p, _p, _p, _p, _p, ctypes.c_size_t, _p])
+_sig("ce_kv_keep", ctypes.c_int, [ctypes.POINTER(CEKVCache), _p, _i32, _p, _p, _p, _p])
+_sig("ce_kv_trim", ctypes.c_int, [ctypes.POINTER(CEKVCache), _p, _p, _p, _p, _p, _p, _p, _p, _p])
+_sig("ce_rotary", ctypes.c_int, [ctypes.POINTER(CERotaryDesc), _p, ctypes.c_int64, _p, ctypes.c_int64, _p])
 _sig("ce_score_tiling", ctypes.c_int, [ctypes.POINTER(CEBatch), ctypes.POINTER(CEScorerW), _p])
 _sig("ce_layer_gap", ctypes.c_int, [ctypes.POINTER(CEBatch), _p, _p, ctypes.c_int, _i32, _p, ctypes.c_float,
                                     _p, _p, _p, _p, _p, _p])
@@ -889,11 +916,7 @@ def alloc_paged_workspace(cache: KVCache, q_rows: int, n_heads: int):
                        device=cache.k.device)
 
 
-def ce_paged_attention(cache: KVCache, q, o, q_offsets, lens, causal, scale, ws=None, stream=None):
-    """q [rows, H, 128] bf16 (rows may be spaced) over the cache's first lens[b] tokens of
-    each sequence, o [rows, H, 128]; q_offsets int32 [B+1], lens int32 [B]. Without
-    a workspace (alloc_paged_workspace) scratch comes from torch's allocator, so a program
-    that captures without torch.cuda.graph passes one of its own."""
+def _paged(cache: KVCache, q, o, q_offsets, lens, causal, mask, scale, ws, stream, where):
     cc = cache.c()
     dev, d, B = cc.device, cc.head_dim, cc.B
     qp, n, h, ld = _rows3(q, "q", dev, d)
@@ -902,18 +925,226 @@ def ce_paged_attention(cache: KVCache, q, o, q_offsets, lens, causal, scale, ws=
     op, no, _, old = _rows3(o, "o", dev, d, h)
     if no < n or old != h * d:
         raise ValueError("o must be contiguous and have q's rows")
+    if mask is not None:
+        mp, words = _mask(mask, dev, n)
     if ws is None:
         need = int(lib.ce_paged_workspace_size(ctypes.byref(cc), ctypes.byref(at)))
         if need:
-            # stream-ordered scratch, on the stream that the kernels run on (any object
-            # with a raw handle is a stream here, as in every call)
-            with torch.cuda.stream(torch.cuda.current_stream() if stream is None else
-                                   stream if isinstance(stream, torch.cuda.Stream) else
-                                   torch.cuda.ExternalStream(stream.cuda_stream)):
-                ws = torch.empty(need, dtype=_U8, device=q.device)
-    _check(lib.ce_paged_attention(ctypes.byref(cc), ctypes.byref(at), qp, ld, op, None if ws is None else _chk(ws, "ws"),
-                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
-           "ce_paged_attention")
+            ws = _scratch(need, q.device, stream)
+    wp, wn = (None, 0) if ws is None else (_chk(ws, "ws"), ws.numel() * ws.element_size())
+    if mask is None:
+        status = lib.ce_paged_attention(ctypes.byref(cc), ctypes.byref(at), qp, ld, op, wp, wn, _stream(stream))
+    else:
+        status = lib.ce_paged_tree_attention(ctypes.byref(cc), ctypes.byref(at), mp, words, qp, ld, op, wp, wn,
+                                             _stream(stream))
+    _check(status, where)
+
+
+def _scratch(need, device, stream):
+    """Stream-ordered scratch, on the stream that the kernels run on (any object with a raw
+    handle is a stream here, as in every call)."""
+    with torch.cuda.stream(torch.cuda.current_stream() if stream is None else
+                           stream if isinstance(stream, torch.cuda.Stream) else
+                           torch.cuda.ExternalStream(stream.cuda_stream)):
+        return torch.empty(need, dtype=_U8, device=device)
+
+
+def _mask(mask, device, rows):
+    """Pointer and words a row of a mask [>= rows, words] of 4-byte integers."""
+    if mask.dim() != 2 or mask.dtype not in (torch.int32, torch.uint32):
+        raise ValueError("mask must be a matrix [rows, words] of 4-byte integers")
+    words = mask.shape[1]
+    if mask.shape[0] < rows:
+        raise ValueError(f"mask has {mask.shape[0]} rows, q {rows}")
+    return _vec(mask, "mask", device, rows * words, mask.dtype), words
+
+
+def ce_paged_attention(cache: KVCache, q, o, q_offsets, lens, causal, scale, ws=None, stream=None):
+    """q [rows, H, 128] bf16 (rows may be spaced) over the cache's first lens[b] tokens of
+    each sequence, o [rows, H, 128]; q_offsets int32 [B+1], lens int32 [B]. Without
+    a workspace (alloc_paged_workspace) scratch comes from torch's allocator, so a program
+    that captures without torch.cuda.graph passes one of its own."""
+    _paged(cache, q, o, q_offsets, lens, causal, None, scale, ws, stream, "ce_paged_attention")
+
+
+# ----------------------------------------------------------------------------
+# drafted decoding over the paged cache (include/ce_router_draft.h)
+# ----------------------------------------------------------------------------
+
+@dataclass
+class Drafts:
+    """The trees of a step: offsets int32 [B+1]; parents int32 [rows] within the sequence, -1
+    for none (None: chains); tokens int32 [rows] (ce_verify_drafts only). Row 0 of a sequence
+    is its last accepted token. `rows`: the host's bound on them where neither parents nor tokens says it."""
+    offsets: "object"
+    parents: "object" = None
+    tokens: "object" = None
+    rows: Optional[int] = None
+
+    def c(self) -> CEDrafts:
+        if self.offsets is None or self.offsets.dim() != 1:
+            raise ValueError("offsets must be a vector [B+1]")
+        op = _chk(self.offsets, "offsets", _I32, 2)
+        dev = _device()
+        sized = self.parents if self.parents is not None else self.tokens
+        if self.rows is None and sized is None:
+            raise ValueError("rows must be given where neither parents nor tokens is")
+        rows = sized.numel() if self.rows is None else int(self.rows)
+        return CEDrafts(self.offsets.numel() - 1, rows, op,
+                        None if self.parents is None else _vec(self.parents, "parents", dev, rows),
+                        None if self.tokens is None else _vec(self.tokens, "tokens", dev, rows))
+
+
+def ce_draft_masks(drafts: Drafts, mask=None, positions=None, base=None, status=None, stream=None):
+    """Bits of every row and its ancestors into mask [rows, words] (int32 or uint32, 1 to 64
+    words), base[b] + the number of ancestors into positions int32 [rows]; status: 4-byte
+    integer tensor for the CE_DEV_* bits."""
+    dc, dev = drafts.c(), _device()
+    rows = dc.row_capacity
+    mp, words = (None, 1) if mask is None else _mask(mask, dev, rows)
+    if status is not None and status.dtype not in (torch.int32, torch.uint32):
+        raise ValueError("status must be a 4-byte integer tensor")
+    _check(lib.ce_draft_masks(ctypes.byref(dc), words, None if base is None else _vec(base, "base", dev, dc.B), mp,
+                              None if positions is None else _vec(positions, "positions", dev, rows),
+                              None if status is None else _vec(status, "status", dev, 1, status.dtype),
+                              _stream(stream)), "ce_draft_masks")
+
+
+def ce_paged_tree_attention(cache: KVCache, q, o, q_offsets, lens, mask, scale, ws=None, stream=None):
+    """ce_paged_attention under a mask of bits [>= rows, words] (ce_draft_masks): a sequence's
+    tokens before its new ones are seen by all its queries, new token j by those whose bit j is set."""
+    if mask is None:
+        raise ValueError("mask must be a matrix [rows, words] of 4-byte integers")
+    _paged(cache, q, o, q_offsets, lens, False, mask, scale, ws, stream, "ce_paged_tree_attention")
+
+
+def ce_verify_workspace_size(drafts: Drafts, vocab: int, with_probs: bool = True) -> int:
+    dc = drafts.c()
+    return int(lib.ce_verify_workspace_size(ctypes.byref(dc), int(vocab), int(bool(with_probs))))
+
+
+def alloc_verify_workspace(drafts: Drafts, vocab: int, with_probs: bool = True):
+    """Workspace of ce_verify_drafts, on the device of the trees."""
+    return torch.empty(max(ce_verify_workspace_size(drafts, vocab, with_probs), 256), dtype=_U8, device=drafts.offsets.device)
+
+
+def _matrix(x, name, device, dtypes, rows, cols=None):
+    """Pointer, columns and stride of a device matrix [>= rows, cols] whose rows may be spaced."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in dtypes:
+        raise ValueError(f"{name} must be a matrix of {' or '.join(map(str, dtypes))}")
+    if not x.is_cuda or x.get_device() != device:
+        raise ValueError(f"{name}: tensor is on {x.device}, the current device is cuda:{device}")
+    n, c = x.shape
+    if n < rows or (cols is not None and c != cols):
+        raise ValueError(f"{name}: shape {tuple(x.shape)}, expected [{rows}, {'columns' if cols is None else cols}]")
+    ld = x.stride(0) if n > 1 else c
+    if (c > 1 and x.stride(1) != 1) or ld < c:
+        raise ValueError(f"{name}: strides {x.stride()}: only rows may be spaced")
+    return x.data_ptr(), c, ld
+
+
+def ce_verify_drafts(drafts: Drafts, logits, u_sample, kept_rows, n_kept, next_token, temperature=None, draft_probs=None,
+                     u_accept=None, ws=None, stream=None):
+    """Which rows the target accepts (kept_rows int32 [rows], n_kept int32 [B]) and the next
+    token of each sequence (int32 [B]). logits [rows, vocab] bf16 or float32, the target's
+    after each row; temperature float32 [B] or None (1); without draft_probs the drafts were
+    chosen, with them (float32 [rows, vocab], and u_accept) the children of a row were
+    drawn from its row; u_sample, u_accept float32 [rows] in [0, 1). Without a workspace
+    (alloc_verify_workspace) scratch comes from torch's allocator."""
+    dc, dev = drafts.c(), _device()
+    rows, B = dc.row_capacity, dc.B
+    lp, vocab, ld = _matrix(logits, "logits", dev, (torch.bfloat16, _F32), rows)
+    pp, pld = None, 0
+    if draft_probs is not None:
+        pp, _, pld = _matrix(draft_probs, "draft_probs", dev, (_F32,), rows, vocab)
+    if rows and drafts.tokens is None:
+        raise ValueError("the trees need their tokens")
+    if ws is None:
+        need = int(lib.ce_verify_workspace_size(ctypes.byref(dc), vocab, int(pp is not None)))
+        if need:
+            ws = _scratch(need, logits.device, stream)
+    _check(lib.ce_verify_drafts(
+        ctypes.byref(dc), vocab, lp, ld, _dtype_code(logits),
+        None if temperature is None else _vec(temperature, "temperature", dev, B, _F32), pp, pld,
+        None if u_accept is None else _vec(u_accept, "u_accept", dev, rows, _F32), _vec(u_sample, "u_sample", dev, rows, _F32),
+        _vec(kept_rows, "kept_rows", dev, rows), _vec(n_kept, "n_kept", dev, B), _vec(next_token, "next_token", dev, B),
+        None if ws is None else _chk(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
+        "ce_verify_drafts")
+
+
+def ce_kv_keep(cache: KVCache, offsets, start, kept_rows, n_kept, stream=None):
+    """The accepted rows of a step (kept_rows int32 [rows], n_kept int32 [B]) move up behind
+    start[b] (ce_kv_reserve's; -1: none) in the pages."""
+    cc = cache.c()
+    dev, B = cc.device, cc.B
+    rows = kept_rows.numel()
+    _check(lib.ce_kv_keep(ctypes.byref(cc), _vec(offsets, "offsets", dev, B + 1), rows, _vec(start, "start", dev, B),
+                          _vec(kept_rows, "kept_rows", dev, rows), _vec(n_kept, "n_kept", dev, B), _stream(stream)),
+           "ce_kv_keep")
+
+
+def ce_kv_trim(cache: KVCache, lens, start, n_kept, free_pages, free_count, lens_out=None, free_count_out=None, status=None,
+               stream=None):
+    """Lengths after ce_kv_keep, and the pages behind them back on the free stack. lens_out
+    and free_count_out default to lens and free_count (in place)."""
+    cc = cache.c()
+    dev, B = cc.device, cc.B
+    if status is not None and status.dtype not in (torch.int32, torch.uint32):
+        raise ValueError("status must be a 4-byte integer tensor")
+    lp, cp = _vec(lens, "lens", dev, B), _vec(free_count, "free_count", dev, 1)
+    _check(lib.ce_kv_trim(
+        ctypes.byref(cc), lp, _vec(start, "start", dev, B), _vec(n_kept, "n_kept", dev, B),
+        _vec(free_pages, "free_pages", dev, cc.n_pages), cp, lp if lens_out is None else _vec(lens_out, "lens_out", dev, B),
+        cp if free_count_out is None else _vec(free_count_out, "free_count_out", dev, 1),
+        None if status is None else _vec(status, "status", dev, 1, status.dtype), _stream(stream)), "ce_kv_trim")
+
+
+# ----------------------------------------------------------------------------
+# rotary positions (include/ce_router_rotary.h)
+# ----------------------------------------------------------------------------
+
+def rotary_freqs(rotary_dim: int, base: float = 10000.0):
+    """Radians a position of each pair of the first rotary_dim values of a head: base^(-2 i / rotary_dim)."""
+    return [float(base) ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)]
+
+
+class Rotary:
+    """How heads are turned: freqs[i] radians a position for pair i, axes[i] the axis of positions
+    that it turns by (None: the first), pairs of neighbours (`interleaved`) or of halves."""
+
+    def __init__(self, freqs: Sequence[float], axes: Optional[Sequence[int]] = None, interleaved: bool = False):
+        if axes is not None and len(axes) != len(freqs):
+            raise ValueError("axes and freqs must have equal length")
+        self.n_pairs, self.interleaved = len(freqs), bool(interleaved)
+        self.n_axes = 1 if axes is None else max(axes, default=0) + 1
+        self._freq = (ctypes.c_double * max(self.n_pairs, 1))(*freqs)
+        self._axis = None if axes is None else (_i32 * max(self.n_pairs, 1))(*axes)
+
+
+def ce_rotary(rotary: Rotary, x, y, positions, index=None, inverse=False, stream=None):
+    """x [rows, heads, head_dim] bf16 or float32 (rows may be spaced, as in a fused projection)
+    turned into y (which may be x); positions int32 [n_positions] or [axes, n_positions];
+    index int32 [rows]: the token of each row (ce_topk_compact's kept_idx), default the row's
+    number. inverse: turned back, the gradient of the turn."""
+    if x is None or x.dim() != 3 or y is None or y.shape != x.shape:
+        raise ValueError("x and y must be [rows, heads, head_dim] of one shape")
+    rows, heads, d = x.shape
+    code = _dtype_code(x)
+    xp, yp = (_chk_strided(t, name, x.dtype, (d, 1), 8) for name, t in (("x", x), ("y", y)))
+    xl, yl = ((t.stride(0) if rows > 1 else -(-heads * d // 8) * 8) for t in (x, y))
+    if positions is None or positions.dim() not in (1, 2):
+        raise ValueError("positions must be [n_positions] or [axes, n_positions]")
+    dev = _device()
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    if axes < rotary.n_axes:
+        raise ValueError(f"positions has {axes} axes, {rotary.n_axes} are turned by")
+    n = positions.shape[-1]
+    desc = CERotaryDesc(rows, heads, d, rotary.n_pairs, axes, CE_ROTARY_PAIRS if rotary.interleaved else CE_ROTARY_HALVES,
+                        int(bool(inverse)), code, n, ctypes.cast(rotary._freq, _p).value,
+                        None if rotary._axis is None else ctypes.cast(rotary._axis, _p).value,
+                        _vec(positions, "positions", dev, axes * n),
+                        None if index is None else _vec(index, "index", dev, rows))
+    _check(lib.ce_rotary(ctypes.byref(desc), xp, xl, yp, yl, _stream(stream)), "ce_rotary")
 
 
 __all__ = [
@@ -929,4 +1160,7 @@ __all__ = [
     "CE_F32", "CE_BF16", "CE_TOK_GEN", "CE_TOK_KEEP", "CE_WS_TOPK", "CE_WS_FFN", "CE_WS_BLOCK", "CE_WS_BLOCK_GAP",
     "CE_WS_FFN_PRUNED", "CE_WS_SCORE",
     "CE_DEV_BAD_OFFSETS", "CE_DEV_OVERFLOW",
+    "Drafts", "ce_draft_masks", "ce_paged_tree_attention", "ce_verify_drafts", "ce_verify_workspace_size",
+    "alloc_verify_workspace", "ce_kv_keep", "ce_kv_trim", "CE_DEV_BAD_TREE", "CE_DEV_TOO_WIDE",
+    "Rotary", "rotary_freqs", "ce_rotary", "CE_ROTARY_HALVES", "CE_ROTARY_PAIRS",
 ]

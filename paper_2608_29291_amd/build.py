@@ -27,7 +27,7 @@ ARCH = "gfx950"
 
 SOURCES = ["ce_api.hip", "ce_score.hip", "ce_topk.hip", "ce_ffn.hip", "ce_ffn_few.hip", "ce_ffn_mid.hip", "ce_scatter.hip", "ce_stability.hip",
            "ce_ucs_ffn.hip", "ce_layer_gap.hip", "ce_attention.hip", "ce_attention_decode.hip", "ce_kv_cache.hip",
-           "ce_paged_attention.hip", "ce_paged_api.hip", "ce_host.cpp"]
+           "ce_paged_attention.hip", "ce_paged_api.hip", "ce_draft.hip", "ce_verify.hip", "ce_rotary.hip", "ce_host.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}"]
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,220 @@
+// Bookkeeping of drafted decoding (include/ce_router_draft.h): masks of trees, and the accepted
+// rows of a step in the paged cache.
+//
+// Masks. Row i sees itself and its ancestors: a walk along the parents, one thread a row, over
+// parents in LDS.
+//
+// Keep. Token start + j becomes token start + r_j with r_0 < r_1 < ..., so r_j >= j: what is
+// written has been read before, as long as the rows are moved in order. A thread moves
+// 16 bytes of a head of every row, eight rows loaded before the first is stored, and no
+// other thread touches its bytes: no barrier, no copy.
+//
+// Trim. As ce_kv_reserve's pages of handed-on sequences: one workgroup, a prefix sum of the pages
+// that come back, dealt to threads by a search in it.
+#include "ce_device.hpp"
+#include "ce_draft.hpp"
+#include "ce_scan.hpp"
+
+namespace ce {
+
+namespace {
+
+using namespace scan;
+
+// A parent is before its row, or there is none (-1).
+__device__ __forceinline__ int parent_of(int p, int i) { return p < 0 || p >= i ? -1 : p; }
+
+constexpr int kStaged = 8192;  // parents that LDS holds
+
+__global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
+  __shared__ int16_t up[kStaged];
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int lo = clampi(a.offs[b], 0, a.rows);
+  const int n = clampi(a.offs[b + 1], lo, a.rows) - lo;
+  const bool staged = n <= kStaged;
+  if (a.parents && staged) {
+    for (int i = tid; i < n; i += 256) up[i] = (int16_t)parent_of(a.parents[lo + i], i);
+    __syncthreads();
+  }
+  const int base = a.base ? a.base[b] : 0;
+  for (int i = tid; i < n; i += 256) {
+    uint32_t* const row = a.mask ? a.mask + (int64_t)(lo + i) * a.words : nullptr;
+    int w = a.words - 1, depth = -1;
+    uint32_t bits = 0;
+    // ancestors come in falling order, so the words are finished one after another
+    for (int j = i; j >= 0;) {
+      ++depth;
+      const int wj = j >> 5;
+      if (row && wj < a.words) {
+        while (w > wj) {
+          row[w--] = bits;
+          bits = 0;
+        }
+        bits |= 1u << (j & 31);
+      }
+      j = !a.parents ? j - 1 : (staged ? (int)up[j] : parent_of(a.parents[lo + j], j));
+    }
+    if (row)
+      for (; w >= 0; --w) {
+        row[w] = bits;
+        bits = 0;
+      }
+    if (a.positions) a.positions[lo + i] = (int)((uint32_t)base + (uint32_t)depth);
+  }
+}
+
+// CE_DEV_* bits of the trees. One workgroup.
+__global__ __launch_bounds__(1024) void draft_status_kernel(DraftMaskArgs a) {
+  __shared__ uint32_t st_s;
+  if (threadIdx.x == 0) st_s = 0;
+  __syncthreads();
+  uint32_t st = 0;
+  for (int b = threadIdx.x; b < a.B; b += 1024) {
+    const int o0 = a.offs[b], o1 = a.offs[b + 1];
+    if (o0 < 0 || o1 < o0 || (b == 0 && o0 != 0)) st |= CE_DEV_BAD_OFFSETS;
+    if (o0 > a.rows || o1 > a.rows) st |= CE_DEV_OVERFLOW;
+    const int lo = clampi(o0, 0, a.rows), n = clampi(o1, lo, a.rows) - lo;
+    if (a.mask && n > 32 * a.words) st |= CE_DEV_TOO_WIDE;
+  }
+  if (a.parents)
+    for (int b = threadIdx.x >> 6; b < a.B; b += 16) {
+      const int lo = clampi(a.offs[b], 0, a.rows), n = clampi(a.offs[b + 1], lo, a.rows) - lo;
+      for (int i = threadIdx.x & 63; i < n; i += 64)
+        if (a.parents[lo + i] >= i) st |= CE_DEV_BAD_TREE;
+    }
+  if (st) atomicOr(&st_s, st);
+  __syncthreads();
+  if (threadIdx.x == 0) *a.status = st_s;
+}
+
+constexpr int kAhead = 8;  // rows in flight in a thread
+
+__global__ __launch_bounds__(256) void kv_keep_kernel(KeepArgs a) {
+  const int b = blockIdx.x >> 1;
+  const bool is_v = blockIdx.x & 1;
+  const int start = a.start[b];
+  const int lo = clampi(a.offs[b], 0, a.rows);
+  const int n = clampi(a.offs[b + 1], lo, a.rows) - lo;
+  const int kept = clampi(a.n_kept[b], 0, n);
+  if (start < 0 || kept == 0) return;
+  char* const pool = is_v ? a.v : a.k;
+  const int32_t* const table = a.table + (int64_t)b * a.max_pages;
+  const int64_t tokens = (int64_t)a.max_pages << a.page_log2;
+  const int mask = (1 << a.page_log2) - 1;
+  auto place = [&](int64_t token, bool& ok) {
+    ok = token < tokens;
+    const int page = ok ? table[token >> a.page_log2] : -1;
+    ok = (uint32_t)page < (uint32_t)a.n_pages;
+    return (int64_t)((uint64_t)(uint32_t)(ok ? page : 0) * a.page_bytes) + (token & mask) * a.row_bytes;
+  };
+  const int pieces = a.row_bytes / 16;
+  for (int c = threadIdx.x; c < a.heads * pieces; c += blockDim.x) {
+    const int h = c / pieces;
+    char* const at = pool + ((int64_t)h << a.page_log2) * a.row_bytes + (c - h * pieces) * 16;
+    int before = -1;
+    for (int j0 = 0; j0 < kept; j0 += kAhead) {
+      u32x4_t x[kAhead];
+      int64_t to[kAhead];
+      bool go[kAhead], good = true;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int j = j0 + i;
+        go[i] = false;
+        if (j >= kept) continue;
+        const int r = a.kept[lo + j];
+        good = good && r > before && r < n;
+        before = r;
+        if (!good || r == j) continue;
+        bool ok0, ok1;
+        const int64_t from = place((int64_t)start + r, ok0);
+        to[i] = place((int64_t)start + j, ok1);
+        go[i] = ok0 && ok1;
+        if (go[i]) x[i] = *reinterpret_cast<const u32x4_t*>(at + from);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (go[i]) *reinterpret_cast<u32x4_t*>(at + to[i]) = x[i];
+      if (!good) break;
+    }
+  }
+}
+
+__global__ __launch_bounds__(1024) void kv_trim_kernel(TrimArgs a) {
+  __shared__ uint32_t scr[32];
+  __shared__ int first[1024], held[1024];
+  __shared__ uint32_t st_s;
+  const int tid = threadIdx.x;
+  if (tid == 0) st_s = 0;
+  const int count0 = *a.count;
+  int count = clampi(count0, 0, a.n_pages);
+  uint32_t st = count != count0 ? CE_DEV_BAD_CACHE : 0;
+  const int most = a.max_pages << a.page_log2;
+  const uint32_t up = (1u << a.page_log2) - 1;
+  for (int s0 = 0; s0 < a.B; s0 += 1024) {
+    const int b = s0 + tid;
+    uint32_t back = 0, none = 0, total, t2;
+    held[tid] = 0;
+    if (b < a.B) {
+      const int len0 = a.lens[b], start = a.start[b], kept = a.n_kept[b];
+      const int len = clampi(len0, 0, most);
+      int now = len;
+      if (start >= 0) now = (int)min((int64_t)len, (int64_t)start + max(kept, 0));
+      if (len != len0 || (start >= 0 && (kept < 0 || (int64_t)start + kept > len))) st |= CE_DEV_BAD_CACHE;
+      a.lens_out[b] = now;
+      held[tid] = (int)(((uint32_t)now + up) >> a.page_log2);
+      back = (((uint32_t)len + up) >> a.page_log2) - (uint32_t)held[tid];
+    }
+    uint32_t to = back;
+    scan2(to, none, total, t2, scr);
+    // (more than the stack has room for is pushed only if pages are held twice)
+    first[tid] = (int)min(to - back, (uint32_t)a.n_pages);
+    const uint32_t room = a.n_pages - count;
+    if (total > room) st |= CE_DEV_BAD_CACHE;
+    const int pushed = (int)min(total, room);
+    __syncthreads();
+    for (int i = tid; i < pushed; i += 1024) {
+      const int k = last_at_most(first, 1024, i);
+      const int page = a.table[(int64_t)(s0 + k) * a.max_pages + held[k] + (i - first[k])];
+      if ((uint32_t)page >= (uint32_t)a.n_pages) st |= CE_DEV_BAD_CACHE;
+      a.free_pages[count + i] = page;
+    }
+    count += pushed;
+    __syncthreads();
+  }
+  if (st) atomicOr(&st_s, st);
+  __syncthreads();
+  if (tid == 0) {
+    *a.count_out = count;
+    if (a.status) *a.status = st_s;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_draft_masks(const DraftMaskArgs& a, hipStream_t stream) {
+  if (a.mask || a.positions) {
+    hipLaunchKernelGGL(draft_masks_kernel, dim3(a.B), dim3(256), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.status) {
+    hipLaunchKernelGGL(draft_status_kernel, dim3(1), dim3(1024), 0, stream, a);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_kv_keep(const KeepArgs& a, hipStream_t stream) {
+  if (a.rows == 0) return hipSuccess;
+  const int columns = a.heads * (a.row_bytes / 16);
+  const int threads = columns >= 256 ? 256 : (columns + 63) / 64 * 64;
+  hipLaunchKernelGGL(kv_keep_kernel, dim3(2 * a.B), dim3(threads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_trim(const TrimArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(kv_trim_kernel, dim3(1), dim3(1024), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace ce

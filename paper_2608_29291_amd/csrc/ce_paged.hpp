@@ -56,6 +56,8 @@ struct PagedArgs {
   unsigned long long* arrived;  // single tokens: counters of the chunks that meet, kPagedPlaces a level
   uint32_t* units;   // else the number of cut units and a record of each, or NULL: none is cut
   unsigned long long token;     // of this call, 48 bits
+  const uint32_t* mask;  // a tree's rows: who sees which new token, mask_words a row; else NULL
+  int mask_words;
   PagedPlan* plan;   // B > kPagedScan: the sequences, then the items, (whole) the chunk length and (slots) if half of the places are filled
 };
 

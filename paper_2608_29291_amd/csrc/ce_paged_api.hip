@@ -1,8 +1,9 @@
-// C entry points of the paged key/value cache (declared in
-// include/ce_router_paged.h): host validation, then the launches.
+// C entry points of the paged key/value cache (declared in include/ce_router_paged.h and
+// include/ce_router_draft.h): host validation, then the launches.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include "ce_draft.hpp"
 #include "ce_host.hpp"
 #include "ce_paged.hpp"
 
@@ -57,6 +58,53 @@ int check_attn(const ce_kv_cache* c, const ce_paged_attn* at) {
 
 PagedGrid grid_of(const ce_kv_cache* c, const ce_paged_attn* at) {
   return paged_grid(c->B, at->n_heads, c->n_kv_heads, at->q_capacity, (int64_t)c->max_pages * c->page_size);
+}
+
+// mask: NULL, or a tree's
+int attend(const ce_kv_cache* cache, const ce_paged_attn* attn, const uint32_t* mask, int32_t mask_words, const void* q,
+           int64_t q_ld, void* o, void* ws, size_t ws_bytes, void* stream) {
+  const int s = check_attn(cache, attn);
+  if (s != CE_OK) return s;
+  if (q_ld < (int64_t)attn->n_heads * 128 || q_ld % 8 != 0) return CE_ERR_INVALID_ARG;
+  if (q_ld >= (int64_t)1 << 22) return CE_ERR_UNSUPPORTED;
+  if (!attn->q_offsets || !attn->lens) return CE_ERR_INVALID_ARG;
+  if (attn->q_capacity > 0 && (!q || !o || !cache->k || !cache->v || !cache->page_table)) return CE_ERR_INVALID_ARG;
+  const PagedGrid p = grid_of(cache, attn);
+  if (p.bytes > 0) {
+    const int e = check_ws(ws, ws_bytes, p.bytes);
+    if (e != CE_OK) return e;
+  }
+  const int elem = cache->dtype == CE_E4M3 ? 1 : 2;
+  PagedArgs a = {};
+  a.q = static_cast<const char*>(q);
+  a.o = static_cast<char*>(o);
+  a.k = static_cast<const char*>(cache->k);
+  a.v = static_cast<const char*>(cache->v);
+  a.ks = cache->k_scale;
+  a.vs = cache->v_scale;
+  a.table = cache->page_table;
+  a.qo = attn->q_offsets;
+  a.lens = attn->lens;
+  a.q_ld = q_ld * 2;
+  a.page_bytes = (uint32_t)(cache->page_stride * elem);
+  a.B = cache->B;
+  a.H = attn->n_heads;
+  a.Hkv = cache->n_kv_heads;
+  a.g = a.H / a.Hkv;
+  a.q_cap = attn->q_capacity;
+  a.n_pages = cache->n_pages;
+  a.max_pages = cache->max_pages;
+  a.page_log2 = log2_of_page(cache->page_size);
+  a.causal = attn->causal;
+  a.mask = mask;
+  a.mask_words = mask_words;
+  a.scale_log2 = attn->scale * 1.4426950408889634f;
+  char* const w = static_cast<char*>(ws);
+  a.plan = reinterpret_cast<PagedPlan*>(w);
+  a.arrived = reinterpret_cast<unsigned long long*>(w + p.plan_bytes);
+  a.units = p.cut_units ? reinterpret_cast<uint32_t*>(w + p.plan_bytes) : nullptr;
+  a.part = reinterpret_cast<float*>(w + p.plan_bytes + p.count_bytes);
+  return hip_status(launch_paged_attention(a, cache->dtype == CE_E4M3, static_cast<hipStream_t>(stream)));
 }
 
 }  // namespace
@@ -126,46 +174,87 @@ size_t ce_paged_workspace_size(const ce_kv_cache* cache, const ce_paged_attn* at
 
 int ce_paged_attention(const ce_kv_cache* cache, const ce_paged_attn* attn, const void* q, int64_t q_ld, void* o,
                        void* ws, size_t ws_bytes, void* stream) {
+  return attend(cache, attn, nullptr, 0, q, q_ld, o, ws, ws_bytes, stream);
+}
+
+int ce_paged_tree_attention(const ce_kv_cache* cache, const ce_paged_attn* attn, const uint32_t* mask, int32_t mask_words,
+                            const void* q, int64_t q_ld, void* o, void* ws, size_t ws_bytes, void* stream) {
   const int s = check_attn(cache, attn);
   if (s != CE_OK) return s;
-  if (q_ld < (int64_t)attn->n_heads * 128 || q_ld % 8 != 0) return CE_ERR_INVALID_ARG;
-  if (q_ld >= (int64_t)1 << 22) return CE_ERR_UNSUPPORTED;
-  if (!attn->q_offsets || !attn->lens) return CE_ERR_INVALID_ARG;
-  if (attn->q_capacity > 0 && (!q || !o || !cache->k || !cache->v || !cache->page_table)) return CE_ERR_INVALID_ARG;
-  const PagedGrid p = grid_of(cache, attn);
-  if (p.bytes > 0) {
-    const int e = check_ws(ws, ws_bytes, p.bytes);
-    if (e != CE_OK) return e;
-  }
+  if (attn->causal != 0 || mask_words < 1 || !mask) return CE_ERR_INVALID_ARG;
+  if (mask_words > 64) return CE_ERR_UNSUPPORTED;
+  return attend(cache, attn, mask, mask_words, q, q_ld, o, ws, ws_bytes, stream);
+}
+
+int ce_draft_masks(const ce_drafts* drafts, int32_t mask_words, const int32_t* base, uint32_t* mask, int32_t* positions,
+                   uint32_t* status, void* stream) {
+  const int s = check_drafts(drafts);
+  if (s != CE_OK) return s;
+  if (mask_words < 1 || !drafts->offsets) return CE_ERR_INVALID_ARG;
+  if (mask_words > 64) return CE_ERR_UNSUPPORTED;
+  DraftMaskArgs a = {};
+  a.B = drafts->B;
+  a.rows = drafts->row_capacity;
+  a.words = mask_words;
+  a.offs = drafts->offsets;
+  a.parents = drafts->parents;
+  a.base = base;
+  a.mask = mask;
+  a.positions = positions;
+  a.status = status;
+  return hip_status(launch_draft_masks(a, static_cast<hipStream_t>(stream)));
+}
+
+int ce_kv_keep(const ce_kv_cache* cache, const int32_t* offsets, int32_t row_capacity, const int32_t* start,
+               const int32_t* kept_rows, const int32_t* n_kept, void* stream) {
+  const int s = check_pages(cache);
+  if (s != CE_OK) return s;
+  if (row_capacity < 0) return CE_ERR_INVALID_ARG;
+  if (row_capacity >= 1 << 24) return CE_ERR_UNSUPPORTED;
+  if (!offsets || !start || !n_kept) return CE_ERR_INVALID_ARG;
+  if (row_capacity > 0 && (!kept_rows || !cache->k || !cache->v || !cache->page_table)) return CE_ERR_INVALID_ARG;
   const int elem = cache->dtype == CE_E4M3 ? 1 : 2;
-  PagedArgs a = {};
-  a.q = static_cast<const char*>(q);
-  a.o = static_cast<char*>(o);
-  a.k = static_cast<const char*>(cache->k);
-  a.v = static_cast<const char*>(cache->v);
-  a.ks = cache->k_scale;
-  a.vs = cache->v_scale;
-  a.table = cache->page_table;
-  a.qo = attn->q_offsets;
-  a.lens = attn->lens;
-  a.q_ld = q_ld * 2;
-  a.page_bytes = (uint32_t)(cache->page_stride * elem);
+  KeepArgs a = {};
   a.B = cache->B;
-  a.H = attn->n_heads;
-  a.Hkv = cache->n_kv_heads;
-  a.g = a.H / a.Hkv;
-  a.q_cap = attn->q_capacity;
+  a.rows = row_capacity;
+  a.heads = cache->n_kv_heads;
+  a.row_bytes = 128 * elem;
   a.n_pages = cache->n_pages;
   a.max_pages = cache->max_pages;
   a.page_log2 = log2_of_page(cache->page_size);
-  a.causal = attn->causal;
-  a.scale_log2 = attn->scale * 1.4426950408889634f;
-  char* const w = static_cast<char*>(ws);
-  a.plan = reinterpret_cast<PagedPlan*>(w);
-  a.arrived = reinterpret_cast<unsigned long long*>(w + p.plan_bytes);
-  a.units = p.cut_units ? reinterpret_cast<uint32_t*>(w + p.plan_bytes) : nullptr;
-  a.part = reinterpret_cast<float*>(w + p.plan_bytes + p.count_bytes);
-  return hip_status(launch_paged_attention(a, cache->dtype == CE_E4M3, static_cast<hipStream_t>(stream)));
+  a.page_bytes = (uint32_t)(cache->page_stride * elem);
+  a.offs = offsets;
+  a.start = start;
+  a.kept = kept_rows;
+  a.n_kept = n_kept;
+  a.table = cache->page_table;
+  a.k = static_cast<char*>(cache->k);
+  a.v = static_cast<char*>(cache->v);
+  return hip_status(launch_kv_keep(a, static_cast<hipStream_t>(stream)));
+}
+
+int ce_kv_trim(const ce_kv_cache* cache, const int32_t* lens, const int32_t* start, const int32_t* n_kept,
+               int32_t* free_pages, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,
+               uint32_t* status, void* stream) {
+  const int s = check_table(cache);
+  if (s != CE_OK) return s;
+  if (!cache->page_table || !lens || !start || !n_kept || !free_pages || !free_count || !lens_out || !free_count_out)
+    return CE_ERR_INVALID_ARG;
+  TrimArgs a = {};
+  a.B = cache->B;
+  a.max_pages = cache->max_pages;
+  a.n_pages = cache->n_pages;
+  a.page_log2 = log2_of_page(cache->page_size);
+  a.lens = lens;
+  a.start = start;
+  a.n_kept = n_kept;
+  a.table = cache->page_table;
+  a.free_pages = free_pages;
+  a.count = free_count;
+  a.lens_out = lens_out;
+  a.count_out = free_count_out;
+  a.status = status;
+  return hip_status(launch_kv_trim(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

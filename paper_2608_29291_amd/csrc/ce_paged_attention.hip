@@ -51,14 +51,14 @@ __device__ __forceinline__ uint32_t item_of(uint32_t w, uint32_t group) {
   return in_xcd / group * (kXcdCount * group) + (w % kXcdCount) * group + in_xcd % group;
 }
 
-template <bool kF8>
+template <bool kF8, bool kTree>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_decode_kernel(PagedArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[kSmem];
   Item it;
-  if (find_item<false>(a, blockIdx.x, it)) paged_few<kF8, true>(a, smem, it);
+  if (find_item<false>(a, blockIdx.x, it)) paged_few<kF8, true, kTree>(a, smem, it);
 }
 
-template <bool kF8>
+template <bool kF8, bool kTree>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_attention_kernel(PagedArgs a,
                                                                                                         uint32_t group) {
   __shared__ __attribute__((aligned(1024))) char smem[kSmem];
@@ -66,9 +66,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   if (!find_item<true>(a, item_of(blockIdx.x, group), it)) return;
   if (it.record >= 0 && it.c == 0 && threadIdx.x == 0) write_record(a, it);
   if (it.few)
-    paged_few<kF8, false>(a, smem, it);
+    paged_few<kF8, false, kTree>(a, smem, it);
   else
-    paged_tile<kF8>(a, smem, it);
+    paged_tile<kF8, kTree>(a, smem, it);
 }
 
 // The plan of more than kPagedScan sequences. One workgroup.
@@ -177,6 +177,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
 // caches. Workgroup (unit, y): the 32 rows y % 4 of a 128-row tile, as that wave of
 // its chunks' workgroups left them (of 16 parts, a quarter of their values); of a few
 // rows, eight.
+template <bool kTree>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
   Item it;
   read_record(a, blockIdx.x, it);  // (any content behind the last, and not used)
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
     if (r >= it.rows) return;
     const int row = it.tile * tile_rows(it.few) + r;
     const int qi = row / g;
-    const float inv = normalizer(l, row_limit(a, it, qi, it.nk) > 0);
+    const float inv = normalizer(l, row_sees<kTree>(a, it, qi, l));
     char* const o = a.o + ((int64_t)(it.qbase + qi) * a.H + it.kvh * g + (row - qi * g)) * kRowB;
 #pragma unroll
     for (int v = 0; v < kN; ++v)
@@ -310,26 +311,27 @@ hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   const dim3 blocks((unsigned)grid), threads(256);
-  if (p.decode) {
-    if (e4m3)
-      hipLaunchKernelGGL(paged_decode_kernel<true>, blocks, threads, 0, stream, a);
-    else
-      hipLaunchKernelGGL(paged_decode_kernel<false>, blocks, threads, 0, stream, a);
+  auto launch = [&](auto f8, auto tree) {
+    constexpr bool kF8 = decltype(f8)::value, kTree = decltype(tree)::value;
+    if (p.decode) {
+      hipLaunchKernelGGL((paged_decode_kernel<kF8, kTree>), blocks, threads, 0, stream, a);
+      return hipGetLastError();
+    }
+    hipLaunchKernelGGL((paged_attention_kernel<kF8, kTree>), blocks, threads, 0, stream, a, group);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.cut_units == 0) return e;
+    // Few units have many chunks: four times as many workgroups read sixteen of them at
+    // a time (8 / 1 heads, five sequences of 6 to 9 tokens over 111 to 11538 keys 23.9,
+    // 19.4 us; 40 of 2 to 9, 12 / 2 heads, up to 11349, 29.3, 25.7). With more units that
+    // costs what it gains (two chunks of 701 beside 30 tokens 36.0, 37.2).
+    const int parts = p.cut_units <= 128 ? 16 : 4;
+    hipLaunchKernelGGL(paged_combine_kernel<kTree>, dim3(p.cut_units, parts), threads, 0, stream, a);
     return hipGetLastError();
-  }
-  if (e4m3)
-    hipLaunchKernelGGL(paged_attention_kernel<true>, blocks, threads, 0, stream, a, group);
-  else
-    hipLaunchKernelGGL(paged_attention_kernel<false>, blocks, threads, 0, stream, a, group);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.cut_units == 0) return e;
-  // Few units have many chunks: four times as many workgroups read sixteen of them at
-  // a time (8 / 1 heads, five sequences of 6 to 9 tokens over 111 to 11538 keys 23.9,
-  // 19.4 us; 40 of 2 to 9, 12 / 2 heads, up to 11349, 29.3, 25.7). With more units that
-  // costs what it gains (two chunks of 701 beside 30 tokens 36.0, 37.2).
-  const int parts = p.cut_units <= 128 ? 16 : 4;
-  hipLaunchKernelGGL(paged_combine_kernel, dim3(p.cut_units, parts), threads, 0, stream, a);
-  return hipGetLastError();
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if (a.mask) return e4m3 ? launch(Yes{}, Yes{}) : launch(No{}, Yes{});
+  return e4m3 ? launch(Yes{}, No{}) : launch(No{}, No{});
 }
 
 }  // namespace ce

@@ -180,6 +180,49 @@ __device__ __forceinline__ int row_limit(const PagedArgs& a, const Item& it, int
   return clampi(it.nk - it.nq + qi + 1, 0, end);
 }
 
+// Under a mask of bits (kTree) a row sees the keys before the sequence's new ones, and of new key j
+// bit j of its words. A block of 32 keys from offset `off` among the new ones (negative: before
+// them) meets words off / 32 and the next, shifted; `left` of its keys exist.
+__device__ __forceinline__ uint32_t block_bits(uint32_t lo, uint32_t hi, int off, int left) {
+  const uint32_t x = __builtin_amdgcn_alignbit(hi, lo, (uint32_t)off & 31);
+  return left >= 32 ? x : (left <= 0 ? 0u : x & ((1u << left) - 1));
+}
+
+// A lane's row of the mask, in vector registers (no scalar ones are left).
+struct MaskRow {
+  const uint32_t* row;
+  int words, first;  // first: the first new key
+  __device__ __forceinline__ uint32_t word(int w) const { return w < 0 ? ~0u : (w < words ? row[w] : 0u); }
+  __device__ __forceinline__ bool sees(int key) const {
+    const int off = key - first;
+    return (word(off >> 5) >> (off & 31)) & 1;
+  }
+};
+template <bool kTree>
+__device__ __forceinline__ MaskRow mask_row(const PagedArgs& a, const Item& it, int qi) {
+  MaskRow m = {nullptr, 0, 0};
+  if constexpr (kTree) {
+    m = MaskRow{a.mask + (int64_t)(it.qbase + qi) * a.mask_words, a.mask_words, it.nk - it.nq};
+    asm volatile("" : "+v"(m.words), "+v"(m.first));
+  }
+  return m;
+}
+
+// Does query qi, whose weights add up to l, see any key?
+template <bool kTree>
+__device__ __forceinline__ bool row_sees(const PagedArgs& a, const Item& it, int qi, float l) {
+  if constexpr (!kTree) return row_limit(a, it, qi, it.nk) > 0;
+  if (l != 0.0f || it.nk > it.nq) return true;  // (NaN too)
+  const uint32_t* const row = a.mask + (int64_t)(it.qbase + qi) * a.mask_words;
+  const int lo = it.nq - it.nk;  // the first bit that stands for a key
+  for (int w = lo >> 5; w < a.mask_words && 32 * w < it.nq; ++w) {
+    uint32_t x = block_bits(row[w], 0, 0, it.nq - 32 * w);
+    if (32 * w < lo) x &= ~0u << (lo & 31);
+    if (x) return true;
+  }
+  return false;
+}
+
 // Inclusive prefix sum over the wave (row shifts, then the rows' last lanes).
 __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
@@ -566,9 +609,11 @@ __device__ __forceinline__ int64_t page_at(const PagedArgs& a, int kvh, int page
 // lane's row sees those below vis. qf: the row, 8 dims a chunk, chunk s from dim
 // 8 (2 s + lane / 32), or with kWide from 16 (2 (s / 2) + lane / 32) + 8 (s % 2). Slow, and
 // reached only where a value is NaN or infinite in a sequence's last rows.
-template <bool kF8, bool kWide>
+// kTree: and that `row` shows.
+template <bool kF8, bool kWide, bool kTree>
 __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, const u32x4_t (&qf)[8], f32x16_t (&oacc)[4],
-                                        float& m, float& l, float c2, int vis, int k0, int kstep, int vis1) {
+                                        float& m, float& l, float c2, int vis, int k0, int kstep, int vis1,
+                                        const MaskRow& row) {
   int lhalf = (threadIdx.x >> 5) & 1;
   asm volatile("" : "+v"(lhalf));  // no address of this path is formed before it
   const int mask = (1 << a.page_log2) - 1;
@@ -602,7 +647,9 @@ __device__ __forceinline__ void paged_redo(const PagedArgs& a, int b, int kvh, c
         __builtin_amdgcn_sched_barrier(0);  // (few registers are left)
       }
       sc += __shfl_xor(sc, 32);
-      if (j < vis) {
+      bool sees = j < vis;
+      if constexpr (kTree) sees = sees && row.sees(j);
+      if (sees) {
         const float m_new = fmaxf(m, sc);
         if (m_new > m) {
           const float al = weight(m, m_new, c2);
@@ -669,7 +716,7 @@ __device__ __forceinline__ uint32_t vt_off(int d, uint32_t u) {
 //   * 8-bit: K straight to registers in operand order (a line in four loads as well,
 //     but half the bytes: 64 tokens over 2100 to 16001 keys 78 us, 4.95 TB/s), V through
 //     registers, converted, exactly, and stored transposed in LDS.
-template <bool kF8, bool kDecode>
+template <bool kF8, bool kDecode, bool kTree>
 __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, const Item& it) {
   float* const ml = reinterpret_cast<float*>(smem + 4 * kFew * kOLd * 4);  // [2][4][kFew]
   const int tid = threadIdx.x;
@@ -711,8 +758,16 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     }
   }
   const int vis = row_limit(a, it, qi, kend);              // keys [0, vis) are seen
-  const int vis0 = row_limit(a, it, q0, kend);             // by the first row
+  const int vis0 = kTree ? clampi(it.nk - it.nq, 0, kend) : row_limit(a, it, q0, kend);  // by the first row (or every one)
   const int vis1 = min(it.vis_end, kend);                  // and by the last
+  const MaskRow mrow = mask_row<kTree>(a, it, qi);
+  uint32_t word0 = 0;   // of the mask; as a rule the only one: 32 rows, so 32 new keys at most
+  uint32_t some = ~0u;  // bit r: row r sees some key
+  if constexpr (kTree) {
+    word0 = mrow.row[0];
+    some = (uint32_t)__builtin_amdgcn_ballot_w64(row_sees<true>(a, it, qi, 0.0f));
+    asm volatile("" : "+v"(some));
+  }
 
   char* const vt = smem + wave * (kF8 ? kVTile : 2 * kVTile);  // bf16: K tile, then V tile
   typedef __attribute__((address_space(3))) char lds_char;
@@ -855,9 +910,18 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     }
     sc += s2;
     if (k0 + kBK > vis0) {
+      if constexpr (kTree) {
+        const int off = k0 - mrow.first, w = off >> 5;
+        const uint32_t lo = w == 0 ? word0 : mrow.word(w), hi = w == -1 ? word0 : mrow.word(w + 1);
+        const uint32_t bits = block_bits(lo, hi, off, vis - k0) >> (4 * lhalf);
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (k0 + 8 * (v >> 2) + 4 * lhalf + (v & 3) >= vis) sc[v] = -__builtin_inff();
+        for (int v = 0; v < 16; ++v)
+          if (!(bits >> (8 * (v >> 2) + (v & 3)) & 1)) sc[v] = -__builtin_inff();
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (k0 + 8 * (v >> 2) + 4 * lhalf + (v & 3) >= vis) sc[v] = -__builtin_inff();
+      }
     }
     // online softmax (lane = row; its keys sit in the lane and in lane ^ 32)
     float mt = sc[0];
@@ -940,7 +1004,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
     }
   }
   if (vis0 < vis1 && any_nan(oacc))
-    paged_redo<kF8, kF8>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg + wave * kBK, step, vis1);
+    paged_redo<kF8, kF8, kTree>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg + wave * kBK, step, vis1, mrow);
 
   // ---- the four waves meet: common maximum, scaled outputs through LDS ----
   int tid_e = threadIdx.x;
@@ -971,7 +1035,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   const __amdgpu_buffer_rsrc_t prs = part_rsrc<kDecode>(a);
   auto finish = [&](int r, const f32x4_t& x, float l) __attribute__((always_inline)) {
     const int q2 = small_div(h0 + r, 1.0f / (float)g);
-    const float inv = normalizer(l, row_limit(a, it, q0 + q2, it.nk) > 0);
+    const float inv = normalizer(l, kTree ? (some >> r & 1) != 0 : row_limit(a, it, q0 + q2, it.nk) > 0);
     store4<true>(a.o + ((int64_t)(it.qbase + q0 + q2) * a.H + kvh * g + (h0 + r - q2 * g)) * kRowB + 8 * qd, x[0] * inv * vs,
                  x[1] * inv * vs, x[2] * inv * vs, x[3] * inv * vs);
   };
@@ -1081,7 +1145,7 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
 // to 10240 keys, 28 heads, causal: 887 us, 1.07 PFLOP/s, MFMA busy 65% of the time
 // and VALU 60%; 4 x 2176 queries over 2304 keys, 12 heads: 134 us, 0.92). 64 rows a
 // wave, with half the LDS reads, leave one wave a SIMD: 986 and 161.
-template <bool kF8>
+template <bool kF8, bool kTree>
 __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem, const Item& it) {
   // Beside other arrays in LDS the compiler ties the DMAs to the fragment reads and
   // drains them before each stage, unless their base passes through an empty asm.
@@ -1210,7 +1274,15 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   bool far = false;     // that of some row is far
   const int qi = q0 + small_div(h0 + min(32 * wave + lrow, it.rows - 1), inv_g);  // this lane's query
   const int vis = row_limit(a, it, qi, kend);  // keys [0, vis) are seen
-  const int vis0 = row_limit(a, it, __builtin_amdgcn_readfirstlane(qi), kend);  // by the wave's first row
+  // by the wave's first row (or every one)
+  const int vis0 =
+      kTree ? clampi(it.nk - it.nq, 0, kend) : row_limit(a, it, __builtin_amdgcn_readfirstlane(qi), kend);
+  const MaskRow mrow = mask_row<kTree>(a, it, qi);
+  int some = 1;  // does the lane's row see any key?
+  if constexpr (kTree) {
+    some = row_sees<true>(a, it, qi, 0.0f);
+    asm volatile("" : "+v"(some));
+  }
 
   using B0 = std::integral_constant<int, 0>;
   using B1 = std::integral_constant<int, 1>;
@@ -1228,9 +1300,17 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   auto mask = [&](int blk, f32x16_t& sc, float& mt) __attribute__((always_inline)) {
     const int kbase = kbeg + blk * kBK;
     if (kbase + kBK > vis0) {
+      if constexpr (kTree) {
+        const int off = kbase - mrow.first, w = off >> 5;
+        const uint32_t bits = block_bits(mrow.word(w), mrow.word(w + 1), off, vis - kbase) >> (4 * lhalf);
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (kbase + 8 * (v >> 2) + 4 * lhalf + (v & 3) >= vis) sc[v] = -__builtin_inff();
+        for (int v = 0; v < 16; ++v)
+          if (!(bits >> (8 * (v >> 2) + (v & 3)) & 1)) sc[v] = -__builtin_inff();
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (kbase + 8 * (v >> 2) + 4 * lhalf + (v & 3) >= vis) sc[v] = -__builtin_inff();
+      }
       mt = tile_max(sc);
     }
   };
@@ -1444,8 +1524,8 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
 #pragma unroll
     for (int j = 8; j < 16; ++j) mfma_step<true>(oacc[j & 3], frag(j, 0, 1), pb[(j - 8) >> 2]);
     const int last_key = min(kend, kbeg + ntiles * kKT);
-    if (a.causal && vis0 < last_key && any_nan(oacc)) {
-      paged_redo<kF8, false>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg, kBK, last_key);
+    if ((kTree || a.causal) && vis0 < last_key && any_nan(oacc)) {
+      paged_redo<kF8, false, kTree>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg, kBK, last_key, mrow);
       if (lhalf) l_run = 0.0f;  // (the whole sum, once)
     }
   }
@@ -1468,7 +1548,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   // ---- O = O^T / l, turned through LDS into whole rows (256 bytes by 16 lanes).
   //      The wave uses its own 8 KB of the K buffers, which no wave reads after
   //      the last barrier. ----
-  const float inv = normalizer(l_run, row_limit(a, it, qi, it.nk) > 0);
+  const float inv = normalizer(l_run, kTree ? some != 0 : row_limit(a, it, qi, it.nk) > 0);
   const float vs = kF8 && a.vs ? a.vs[kvh] : 1.0f;
   char* const ob = kbuf + wave * 32 * kRowB;
 #pragma unroll
