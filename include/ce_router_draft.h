@@ -95,7 +95,8 @@ int ce_paged_tree_attention(const ce_kv_cache* cache, const ce_paged_attn* attn,
  *     asked. Where the walk ends the next token is sampled from max(p_r - c q_r, 0) / S
  *     (from p_r if S is 0).
  *   A sample of weights w by u is the first i with w_0 + .. + w_i > u (w_0 + .. + w_(vocab-1)),
- *   the last i of a positive weight where rounding leaves none.
+ *   the last i of a positive weight where rounding leaves none. Weights below 2^-800 of a
+ *   row's largest count as none.
  *   T is not positive (or NaN): p_r is 1 at the lowest index of the largest logit.
  * Logits of NaN count as -infinity; where some are +infinity they share all probability. A row
  * without a logit above -infinity has no distribution: its walk ends there, without a next

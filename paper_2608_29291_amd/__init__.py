@@ -1117,8 +1117,32 @@ class Rotary:
             raise ValueError("axes and freqs must have equal length")
         self.n_pairs, self.interleaved = len(freqs), bool(interleaved)
         self.n_axes = 1 if axes is None else max(axes, default=0) + 1
-        self._freq = (ctypes.c_double * max(self.n_pairs, 1))(*freqs)
-        self._axis = None if axes is None else (_i32 * max(self.n_pairs, 1))(*axes)
+        self.layout = CE_ROTARY_PAIRS if interleaved else CE_ROTARY_HALVES
+        self._arrays = (ctypes.c_double * max(self.n_pairs, 1))(*freqs), (_i32 * max(self.n_pairs, 1))(*(axes or ()))
+        self.freq_ptr = ctypes.addressof(self._arrays[0])
+        self.axis_ptr = None if axes is None else ctypes.addressof(self._arrays[1])
+
+    def __reduce__(self):
+        """By values: the pointers are of this process's memory."""
+        n = self.n_pairs
+        return Rotary, (list(self._arrays[0][:n]), None if self.axis_ptr is None else list(self._arrays[1][:n]),
+                        self.interleaved)
+
+
+def _spaced(x, name, dtype, heads, d):
+    """Pointer of rows [n, heads, d] that may be spaced, and their stride in elements."""
+    try:
+        p = x.data_ptr()
+        if x.dtype is dtype and x.get_device() == _device() and not p & 15:
+            row = heads * d
+            if x.is_contiguous() and not row & 7:
+                return p, row
+            s = x.stride()
+            if x.is_cuda and s[2] == 1 and s[1] == d and s[0] >= row and not s[0] & 7:
+                return p, s[0]
+    except (AttributeError, TypeError):
+        pass
+    return _chk_strided(x, name, dtype, (d, 1), 8), x.stride(0) if x.shape[0] > 1 else -(-heads * d // 8) * 8
 
 
 def ce_rotary(rotary: Rotary, x, y, positions, index=None, inverse=False, stream=None):
@@ -1130,8 +1154,8 @@ def ce_rotary(rotary: Rotary, x, y, positions, index=None, inverse=False, stream
         raise ValueError("x and y must be [rows, heads, head_dim] of one shape")
     rows, heads, d = x.shape
     code = _dtype_code(x)
-    xp, yp = (_chk_strided(t, name, x.dtype, (d, 1), 8) for name, t in (("x", x), ("y", y)))
-    xl, yl = ((t.stride(0) if rows > 1 else -(-heads * d // 8) * 8) for t in (x, y))
+    xp, xl = _spaced(x, "x", x.dtype, heads, d)
+    yp, yl = _spaced(y, "y", x.dtype, heads, d)
     if positions is None or positions.dim() not in (1, 2):
         raise ValueError("positions must be [n_positions] or [axes, n_positions]")
     dev = _device()
@@ -1139,10 +1163,8 @@ def ce_rotary(rotary: Rotary, x, y, positions, index=None, inverse=False, stream
     if axes < rotary.n_axes:
         raise ValueError(f"positions has {axes} axes, {rotary.n_axes} are turned by")
     n = positions.shape[-1]
-    desc = CERotaryDesc(rows, heads, d, rotary.n_pairs, axes, CE_ROTARY_PAIRS if rotary.interleaved else CE_ROTARY_HALVES,
-                        int(bool(inverse)), code, n, ctypes.cast(rotary._freq, _p).value,
-                        None if rotary._axis is None else ctypes.cast(rotary._axis, _p).value,
-                        _vec(positions, "positions", dev, axes * n),
+    desc = CERotaryDesc(rows, heads, d, rotary.n_pairs, axes, rotary.layout, 1 if inverse else 0, code, n, rotary.freq_ptr,
+                        rotary.axis_ptr, _vec(positions, "positions", dev, axes * n),
                         None if index is None else _vec(index, "index", dev, rows))
     _check(lib.ce_rotary(ctypes.byref(desc), xp, xl, yp, yl, _stream(stream)), "ce_rotary")
 

@@ -1,8 +1,12 @@
 // Bookkeeping of drafted decoding (include/ce_router_draft.h): masks of trees, and the accepted
 // rows of a step in the paged cache.
 //
-// Masks. Row i sees itself and its ancestors: a walk along the parents, one thread a row, over
-// parents in LDS.
+// Masks. Row i sees itself and its ancestors, whose numbers fall. Rows are taken 32 at a time, a word of
+// the masks: five rounds of doubling (m |= m[p], p = p[p], by exchanges in the wave) give a row's
+// ancestors among its 32 and the parent where they leave these, and a walk along these exits,
+// through LDS, meets each word at most once: 22 steps for a chain of 700, not 700. Bound:
+// latency; 16 trees of 26 rows 2.6 us, 253 of 64 and 33 with three chains of 700 and masks of 24 words
+// MASKS_SERVER us (a walk parent by parent 207).
 //
 // Keep. Token start + j becomes token start + r_j with r_0 < r_1 < ..., so r_j >= j: what is
 // written has been read before, as long as the rows are moved in order. A thread moves
@@ -24,42 +28,80 @@ using namespace scan;
 // A parent is before its row, or there is none (-1).
 __device__ __forceinline__ int parent_of(int p, int i) { return p < 0 || p >= i ? -1 : p; }
 
-constexpr int kStaged = 8192;  // parents that LDS holds
+constexpr int kStaged = 8192;  // rows whose words and exits LDS holds
 
 __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
-  __shared__ int16_t up[kStaged];
+  // words of the rows and their exits, `staged` of each, then the masks of 256 rows
+  extern __shared__ uint32_t lds[];
+  uint32_t* const own = lds;
+  int16_t* const out = reinterpret_cast<int16_t*>(lds + a.staged);
+  uint32_t* const tile = lds + a.staged + a.staged / 2;
   const int b = blockIdx.x, tid = threadIdx.x;
   const int lo = clampi(a.offs[b], 0, a.rows);
   const int n = clampi(a.offs[b + 1], lo, a.rows) - lo;
-  const bool staged = n <= kStaged;
-  if (a.parents && staged) {
-    for (int i = tid; i < n; i += 256) up[i] = (int16_t)parent_of(a.parents[lo + i], i);
-    __syncthreads();
-  }
   const int base = a.base ? a.base[b] : 0;
-  for (int i = tid; i < n; i += 256) {
-    uint32_t* const row = a.mask ? a.mask + (int64_t)(lo + i) * a.words : nullptr;
-    int w = a.words - 1, depth = -1;
-    uint32_t bits = 0;
-    // ancestors come in falling order, so the words are finished one after another
-    for (int j = i; j >= 0;) {
-      ++depth;
-      const int wj = j >> 5;
-      if (row && wj < a.words) {
-        while (w > wj) {
-          row[w--] = bits;
-          bits = 0;
-        }
-        bits |= 1u << (j & 31);
-      }
-      j = !a.parents ? j - 1 : (staged ? (int)up[j] : parent_of(a.parents[lo + j], j));
+  // the word of row i, and the parent that it leaves its 32 rows by
+  auto word = [&](int i, uint32_t& m, int& exit) __attribute__((always_inline)) {
+    const int first = i & ~31;
+    const int up = i >= n ? -1 : (a.parents ? parent_of(a.parents[lo + i], i) : i - 1);
+    int p = up >= first ? up & 31 : i & 31;  // (a row without one here points at itself)
+    m = 1u << (i & 31);
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      m |= (uint32_t)__shfl((int)m, p, 32);
+      p = __shfl(p, p, 32);
     }
-    if (row)
-      for (; w >= 0; --w) {
-        row[w] = bits;
-        bits = 0;
+    exit = __shfl(up >= first ? -1 : up, p, 32);
+  };
+  const bool staged = n <= a.staged;
+  if (staged && n > 256) {
+    for (int i0 = 0; i0 < n; i0 += 256) {
+      uint32_t m;
+      int exit;
+      word(i0 + tid, m, exit);
+      if (i0 + tid < n) {
+        own[i0 + tid] = m;
+        out[i0 + tid] = (int16_t)exit;
       }
-    if (a.positions) a.positions[lo + i] = (int)((uint32_t)base + (uint32_t)depth);
+    }
+  }
+  for (int i0 = 0; i0 < n; i0 += 256) {
+    const int i = i0 + tid, rows = min(256, n - i0);
+    uint32_t m;
+    int exit;
+    word(i, m, exit);
+    if (n <= 256) {
+      own[tid] = m;
+      out[tid] = (int16_t)exit;
+    }
+    if (a.mask)
+      for (int k = tid; k < rows * a.words; k += 256) tile[k] = 0;
+    __syncthreads();
+    if (i < n) {
+      int w = i >> 5, depth = -1;
+      for (;;) {
+        depth += __builtin_popcount(m);
+        if (a.mask && w < a.words) tile[tid * a.words + w] = m;
+        if (exit < 0) break;
+        w = exit >> 5;
+        if (staged) {
+          m = own[exit];
+          exit = out[exit];
+        } else {  // a longer sequence than LDS holds: parent by parent
+          m = 0;
+          int j = exit;
+          for (; j >= 0 && j >> 5 == w; j = a.parents ? parent_of(a.parents[lo + j], j) : j - 1) m |= 1u << (j & 31);
+          exit = j;
+        }
+      }
+      if (a.positions) a.positions[lo + i] = (int)((uint32_t)base + (uint32_t)depth);
+    }
+    if (a.mask) {
+      __syncthreads();
+      uint32_t* const to = a.mask + (int64_t)(lo + i0) * a.words;
+      for (int k = tid; k < rows * a.words; k += 256) to[k] = tile[k];
+      __syncthreads();
+    }
   }
 }
 
@@ -191,9 +233,12 @@ __global__ __launch_bounds__(1024) void kv_trim_kernel(TrimArgs a) {
 
 }  // namespace
 
-hipError_t launch_draft_masks(const DraftMaskArgs& a, hipStream_t stream) {
+hipError_t launch_draft_masks(DraftMaskArgs a, hipStream_t stream) {
   if (a.mask || a.positions) {
-    hipLaunchKernelGGL(draft_masks_kernel, dim3(a.B), dim3(256), 0, stream, a);
+    const int staged = a.rows < kStaged ? a.rows : kStaged;
+    a.staged = staged < 256 ? 256 : (staged + 1) / 2 * 2;
+    const size_t lds = (size_t)a.staged * 6 + (a.mask ? (size_t)256 * a.words * 4 : 0);
+    hipLaunchKernelGGL(draft_masks_kernel, dim3(a.B), dim3(256), lds, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -10,6 +10,7 @@ namespace ce {
 
 struct DraftMaskArgs {
   int B, rows, words;
+  int staged;              // rows that LDS holds
   const int32_t* offs;
   const int32_t* parents;  // or NULL: chains
   const int32_t* base;     // or NULL
@@ -35,7 +36,7 @@ struct TrimArgs {
   uint32_t* status;  // or NULL
 };
 
-hipError_t launch_draft_masks(const DraftMaskArgs& a, hipStream_t stream);
+hipError_t launch_draft_masks(DraftMaskArgs a, hipStream_t stream);
 hipError_t launch_kv_keep(const KeepArgs& a, hipStream_t stream);
 hipError_t launch_kv_trim(const TrimArgs& a, hipStream_t stream);
 

@@ -171,12 +171,12 @@ hipError_t launch_by_width(RotaryArgs& a, int n, bool pairs, bool many, hipStrea
   return pairs ? launch<E, 1, true>(a, many, stream) : launch<E, 1, false>(a, many, stream);
 }
 
-// freq / (2 pi) modulo 1 as a 64-bit fraction.
+// freq / (2 pi) modulo 1 as a 64-bit fraction, |freq| <= 64. (64 bits of the long double's mantissa; the
+// fraction's own last bit is left out, which no position makes more than 2^-32 of a turn.)
 uint64_t fraction_of_turn(double freq) {
-  long double v = (long double)freq / 6.283185307179586476925286766559005768L;
-  v -= floorl(v);
-  const long double w = roundl(v * 18446744073709551616.0L);
-  return w >= 18446744073709551616.0L ? 0 : (uint64_t)w;
+  const long double v = (long double)freq * 0.159154943091895335768883763372514362L;
+  const long double part = v - (long double)(int64_t)v;  // of v's sign, below 1
+  return (uint64_t)(int64_t)(part * 9223372036854775808.0L) << 1;
 }
 
 }  // namespace
