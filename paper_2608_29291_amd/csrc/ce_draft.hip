@@ -5,8 +5,8 @@
 // the masks: five rounds of doubling (m |= m[p], p = p[p], by exchanges in the wave) give a row's
 // ancestors among its 32 and the parent where they leave these, and a walk along these exits,
 // through LDS, meets each word at most once: 22 steps for a chain of 700, not 700. Bound:
-// latency; 16 trees of 26 rows 2.6 us, 253 of 64 and 33 with three chains of 700 and masks of 24 words
-// MASKS_SERVER us (a walk parent by parent 207).
+// latency; 16 trees of 26 rows 2.8 us, 253 of 64 and 33 with three chains of 700 and masks of 24 words
+// 6.8 us (a walk parent by parent 207).
 //
 // Keep. Token start + j becomes token start + r_j with r_0 < r_1 < ..., so r_j >= j: what is
 // written has been read before, as long as the rows are moved in order. A thread moves
@@ -31,63 +31,70 @@ __device__ __forceinline__ int parent_of(int p, int i) { return p < 0 || p >= i 
 constexpr int kStaged = 8192;  // rows whose words and exits LDS holds
 
 __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
-  // words of the rows and their exits, `staged` of each, then the masks of 256 rows
+  // words of the rows and their exits, `staged` of each
   extern __shared__ uint32_t lds[];
   uint32_t* const own = lds;
   int16_t* const out = reinterpret_cast<int16_t*>(lds + a.staged);
-  uint32_t* const tile = lds + a.staged + a.staged / 2;
-  const int b = blockIdx.x, tid = threadIdx.x;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int lo = clampi(a.offs[b], 0, a.rows);
   const int n = clampi(a.offs[b + 1], lo, a.rows) - lo;
   const int base = a.base ? a.base[b] : 0;
-  // the word of row i, and the parent that it leaves its 32 rows by
-  auto word = [&](int i, uint32_t& m, int& exit) __attribute__((always_inline)) {
-    const int first = i & ~31;
-    const int up = i >= n ? -1 : (a.parents ? parent_of(a.parents[lo + i], i) : i - 1);
-    int p = up >= first ? up & 31 : i & 31;  // (a row without one here points at itself)
-    m = 1u << (i & 31);
-#pragma unroll
-    for (int k = 0; k < 5; ++k) {
-      m |= (uint32_t)__shfl((int)m, p, 32);
-      p = __shfl(p, p, 32);
-    }
-    exit = __shfl(up >= first ? -1 : up, p, 32);
-  };
   const bool staged = n <= a.staged;
-  if (staged && n > 256) {
-    for (int i0 = 0; i0 < n; i0 += 256) {
-      uint32_t m;
-      int exit;
-      word(i0 + tid, m, exit);
-      if (i0 + tid < n) {
-        own[i0 + tid] = m;
-        out[i0 + tid] = (int16_t)exit;
+  int done = 0;  // rows that are staged
+  // rows 256 y .., and on from there by as many as the workgroups of the sequence take
+  for (int i0 = blockIdx.y * 256; i0 < n; i0 += gridDim.y * 256) {
+    const int i = i0 + tid;
+    uint32_t m = 0;
+    int exit = -1;
+    if (!staged) done = i0;  // (a longer sequence than LDS holds: only the words of these rows)
+    for (int j0 = done; j0 <= i0; j0 += 4 * 256) {
+      int up[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = j0 + 256 * k + tid;
+        up[k] = j < n && j0 + 256 * k <= i0 ? (a.parents ? parent_of(a.parents[lo + j], j) : j - 1) : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (j0 + 256 * k > i0) break;
+        // the word of row j, and the parent that it leaves its 32 rows by
+        const int j = j0 + 256 * k + tid, first = j & ~31;
+        int p = up[k] >= first ? up[k] & 31 : j & 31;  // (a row without one here points at itself)
+        m = 1u << (j & 31);
+#pragma unroll
+        for (int r = 0; r < 5; ++r) {
+          m |= (uint32_t)__shfl((int)m, p, 32);
+          p = __shfl(p, p, 32);
+        }
+        exit = __shfl(up[k] >= first ? -1 : up[k], p, 32);
+        if (staged) {
+          own[j] = m;
+          out[j] = (int16_t)exit;
+        }
       }
     }
-  }
-  for (int i0 = 0; i0 < n; i0 += 256) {
-    const int i = i0 + tid, rows = min(256, n - i0);
-    uint32_t m;
-    int exit;
-    word(i, m, exit);
-    if (n <= 256) {
-      own[tid] = m;
-      out[tid] = (int16_t)exit;
+    done = i0 + 256;
+    // the wave's rows are zeros, and then their words that are none
+    if (a.mask) {
+      const int w0 = i0 + (tid & ~63);
+      uint32_t* const to = a.mask + (int64_t)(lo + w0) * a.words;
+      for (int k = lane; k < min(64, n - w0) * a.words; k += 64) to[k] = 0;
+      asm volatile("" ::: "memory");
+      wait_vmcnt<0>();
     }
-    if (a.mask)
-      for (int k = tid; k < rows * a.words; k += 256) tile[k] = 0;
     __syncthreads();
     if (i < n) {
+      uint32_t* const row = a.mask + (int64_t)(lo + i) * a.words;
       int w = i >> 5, depth = -1;
       for (;;) {
         depth += __builtin_popcount(m);
-        if (a.mask && w < a.words) tile[tid * a.words + w] = m;
+        if (a.mask && w < a.words) row[w] = m;
         if (exit < 0) break;
         w = exit >> 5;
         if (staged) {
           m = own[exit];
           exit = out[exit];
-        } else {  // a longer sequence than LDS holds: parent by parent
+        } else {  // parent by parent
           m = 0;
           int j = exit;
           for (; j >= 0 && j >> 5 == w; j = a.parents ? parent_of(a.parents[lo + j], j) : j - 1) m |= 1u << (j & 31);
@@ -96,12 +103,7 @@ __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
       }
       if (a.positions) a.positions[lo + i] = (int)((uint32_t)base + (uint32_t)depth);
     }
-    if (a.mask) {
-      __syncthreads();
-      uint32_t* const to = a.mask + (int64_t)(lo + i0) * a.words;
-      for (int k = tid; k < rows * a.words; k += 256) to[k] = tile[k];
-      __syncthreads();
-    }
+    __syncthreads();
   }
 }
 
@@ -235,10 +237,11 @@ __global__ __launch_bounds__(1024) void kv_trim_kernel(TrimArgs a) {
 
 hipError_t launch_draft_masks(DraftMaskArgs a, hipStream_t stream) {
   if (a.mask || a.positions) {
-    const int staged = a.rows < kStaged ? a.rows : kStaged;
-    a.staged = staged < 256 ? 256 : (staged + 1) / 2 * 2;
-    const size_t lds = (size_t)a.staged * 6 + (a.mask ? (size_t)256 * a.words * 4 : 0);
-    hipLaunchKernelGGL(draft_masks_kernel, dim3(a.B), dim3(256), lds, stream, a);
+    // (whole passes of 256 rows)
+    a.staged = a.rows < kStaged ? (a.rows + 255) / 256 * 256 : kStaged;
+    const int passes = (a.rows + 255) / 256;
+    const dim3 grid(a.B, passes < 4 ? (passes < 1 ? 1 : passes) : 4);
+    hipLaunchKernelGGL(draft_masks_kernel, grid, dim3(256), (size_t)a.staged * 6, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -140,6 +140,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
   const uint32_t all = (uint32_t)min(base, (int64_t)1 << 30);
   if (whole) w = sum(rest);
   int L = chunk_length(w);
+  bool near = !a.decode && rounds_up(a, L);
   for (;;) {
     const bool half = a.decode && half_places(a, L, all, w_all, most);
     int64_t items = 0, slots = 0, cuts = 0;
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
     for (int b0 = 0; b0 < a.B; b0 += 512) {
       const int b = b0 + tid;
       Counts c = {0, 0, 0};
-      if (b < a.B) c = counts_of(a, size_of(a, b, g), g, L, half, a.plan[b].whole);
+      if (b < a.B) c = counts_of(a, size_of(a, b, g), g, L, half, near, a.plan[b].whole);
       const int64_t i0 = items + scan(c.items, total);
       items += total;
       const int64_t s0 = slots + scan(c.slots, total);
@@ -162,13 +163,14 @@ __global__ __launch_bounds__(512) void paged_plan_kernel(PagedArgs a) {
     }
     if (tid == 0) {
       a.plan[a.B].items = put(items);
-      a.plan[a.B].slots = half;
+      a.plan[a.B].slots = (half ? 1 : 0) | (near ? 2 : 0);
       a.plan[a.B].whole = (uint32_t)L;
       if (a.units) *a.units = put(cuts);
     }
     // (as in find_by_scan)
     if (L == 1 << 30 || (items <= a.grid && slots <= kPagedPlaces)) break;
-    L = 1 << 30;
+    if (!near) L = 1 << 30;
+    near = false;
   }
 }
 

@@ -30,6 +30,7 @@ constexpr int kMaxEven = 1024;     // and where the sequences are about equal
 constexpr int kMaxMeet = 512;      // keys per chunk up to which no more than kMeet meet
 constexpr int kMostOver = 24;      // chunks that are made kMeet whatever their keys
 constexpr int kMinTile = 256;
+constexpr int kWideMask = 4;       // words of a mask from which tiles end where their rows' bits do
 constexpr int kMeet = 16;          // chunks that meet at a time in the launch itself
 constexpr int kOLd = kDh + 4;      // floats per row of paged_few's outputs in LDS
 constexpr int kVRow = kBK * 2;     // bytes per row of paged_few's V^T
@@ -73,6 +74,11 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 //     unequal ones need the finer cut there (half as many / this: 57, 31, 43 and 48
 //     drawn sequences 38 / 29, 56 / 46, 40 / 27, 68 / 51).
 //
+// Under masks of bits, where L is 512 keys or more, a unit's count is rounded to the nearest, as long as
+// no more than S chunks come of it. Trees of 12 to 40 sequences, lengths of 1000 to 16000 (36 drawn
+// batches): between -15% and +13% of the time, -2.4% on average; 32 trees over 2100 to 16001
+// keys 212 / 176 us, two prompts with images 93 / 97. With a smaller L it costs 1.3%.
+//
 // How the chunks meet: of single tokens, in the launch itself (a second one would
 // cost 4 us of 15); of many rows, by a second launch over the whole chip, since one
 // workgroup would read 64 KB a chunk.
@@ -115,15 +121,21 @@ __device__ __forceinline__ bool half_places(const PagedArgs& a, int L, uint32_t 
   return L <= kMaxHalf / 2 || (L <= kMaxEven / 2 && most * (float)units <= 1.25f * w);
 }
 
+// Are the chunks of tiles counted to the nearest?
+__device__ __forceinline__ bool rounds_up(const PagedArgs& a, int L) { return a.mask && L >= 2 * kMinTile; }
+
 // A sequence's chunks (a whole number of its waves' tiles).
-__device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, bool half, int& C, int& chunk) {
+__device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, bool half, bool near, int& C,
+                                    int& chunk) {
   const bool few = is_few(a, s.nq, g);
   if (few) {
     const int l = 2 * min(L, 1 << 29);  // (2^30: nothing is cut)
     C = s.nk < kWholeFew ? 1 : s.nk / max(half ? 2 * l : l, kMinFew);
     if (C > kMeet && (s.nk <= kMeet * kMaxMeet || C <= kMostOver)) C = kMeet;
   } else {
-    C = s.nk / max(L, kMinTile);
+    const int l = max(L, kMinTile);
+    // (shorter sequences are never cut: the host may have left the workspace out)
+    C = (int)(((uint32_t)s.nk + (near && s.nk >= 2 * kMinTile ? (uint32_t)l / 2 : 0)) / (uint32_t)l);
   }
   chunk = s.nk;
   if (C > 1) {
@@ -153,9 +165,10 @@ struct Counts {
   uint32_t items, slots, cut;
   int C, chunk;
 };
-__device__ __forceinline__ Counts counts_of(const PagedArgs& a, const Size& s, int g, int L, bool half, uint32_t whole) {
+__device__ __forceinline__ Counts counts_of(const PagedArgs& a, const Size& s, int g, int L, bool half, bool near,
+                                             uint32_t whole) {
   Counts c;
-  cut(a, s, g, L, half, c.C, c.chunk);
+  cut(a, s, g, L, half, near, c.C, c.chunk);
   const uint32_t n = (uint32_t)s.tiles * a.Hkv;
   c.cut = c.C > 1 ? n - whole : 0;
   c.slots = c.cut * c.C;
@@ -193,18 +206,24 @@ struct MaskRow {
   const uint32_t* row;
   int words, first;  // first: the first new key
   __device__ __forceinline__ uint32_t word(int w) const { return w < 0 ? ~0u : (w < words ? row[w] : 0u); }
+  // of the 32 keys from `key` on, of which `left` exist
+  __device__ __forceinline__ uint32_t block(int key, int left) const {
+    const int off = key - first, w = off >> 5;
+    return block_bits(word(w), word(w + 1), off, left);
+  }
   __device__ __forceinline__ bool sees(int key) const {
     const int off = key - first;
     return (word(off >> 5) >> (off & 31)) & 1;
   }
 };
-template <bool kTree>
 __device__ __forceinline__ MaskRow mask_row(const PagedArgs& a, const Item& it, int qi) {
-  MaskRow m = {nullptr, 0, 0};
-  if constexpr (kTree) {
-    m = MaskRow{a.mask + (int64_t)(it.qbase + qi) * a.mask_words, a.mask_words, it.nk - it.nq};
-    asm volatile("" : "+v"(m.words), "+v"(m.first));
-  }
+  return MaskRow{a.mask + (int64_t)(it.qbase + qi) * a.mask_words, a.mask_words, it.nk - it.nq};
+}
+
+// The row `mine` behind that which a tile holds in LDS.
+__device__ __forceinline__ MaskRow held_row(const char* smem, int mine) {
+  MaskRow m = *reinterpret_cast<const MaskRow*>(smem + 4 * kKBytes);
+  m.row += (int64_t)mine * m.words;
   return m;
 }
 
@@ -307,6 +326,7 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
     w = wave_sum(rest);
   }
   int L = chunk_length(w);
+  bool near = kRecord && rounds_up(a, L);
   Counts n[kPer];
   uint32_t wh[kPer], sum, sum_s, sum_c, to, slots_to;
   for (;;) {
@@ -316,7 +336,7 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       wh[i] = whole_of(a, s[i], first, whole);
-      n[i] = counts_of(a, s[i], g, L, half, wh[i]);
+      n[i] = counts_of(a, s[i], g, L, half, near, wh[i]);
       first += (uint32_t)s[i].tiles * a.Hkv;
       sum += n[i].items;
       sum_s += n[i].slots;
@@ -324,13 +344,14 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
     }
     slots_to = wave_scan(sum_s);
     to = wave_scan(sum);
-    // more workgroups than the launch has, or slots than the workspace: only where
-    // offsets are out of order. Then nothing is cut (every chunk of a cut unit
+    // more workgroups than the launch has, or slots than the workspace: where counts are
+    // rounded up too many of them were, else only where offsets are out of order. Then nothing is cut (every chunk of a cut unit
     // must run) and what lies past the grid is left.
     if (L == 1 << 30 ||
         (__builtin_amdgcn_readlane(to, 63) <= a.grid && __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedPlaces))
       break;
-    L = 1 << 30;
+    if (!near) L = 1 << 30;
+    near = false;
   }
   uint32_t cut_to = 0;
   if (kRecord && a.units) {
@@ -386,13 +407,13 @@ __device__ __forceinline__ bool find_in_plan(const PagedArgs& a, int g, uint32_t
   f.cut = __builtin_amdgcn_readfirstlane(a.plan[f.b].cut);
   f.whole = __builtin_amdgcn_readfirstlane(a.plan[f.b].whole);
   const int L = __builtin_amdgcn_readfirstlane((int)a.plan[a.B].whole);
-  const bool half = __builtin_amdgcn_readfirstlane(a.plan[a.B].slots) != 0;
+  const uint32_t flags = __builtin_amdgcn_readfirstlane(a.plan[a.B].slots);
   const Size s = size_of(a, f.b, g);
   f.size.qbase = __builtin_amdgcn_readfirstlane(s.qbase);
   f.size.nq = __builtin_amdgcn_readfirstlane(s.nq);
   f.size.nk = __builtin_amdgcn_readfirstlane(s.nk);
   f.size.tiles = __builtin_amdgcn_readfirstlane(s.tiles);
-  cut(a, f.size, g, L, half, f.C, f.chunk);
+  cut(a, f.size, g, L, flags & 1, flags & 2, f.C, f.chunk);
   f.C = __builtin_amdgcn_readfirstlane(f.C);
   f.chunk = __builtin_amdgcn_readfirstlane(f.chunk);
   return true;
@@ -442,6 +463,18 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item&
   const int r0 = it.tile * tile_rows(it.few);
   it.rows = min(tile_rows(it.few), it.nq * g - r0);
   it.vis_end = row_limit(a, it, (r0 + it.rows - 1) / g, it.nk);
+  if (!it.few && a.mask && a.mask_words > kWideMask) {
+    // the last new key that some row of the tile sees (masks of trees are too short for it to pay)
+    const int q0 = r0 / g, words = a.mask_words, n = ((r0 + it.rows - 1) / g - q0 + 1) * words;
+    const uint32_t* const p = a.mask + (int64_t)(it.qbase + q0) * words;
+    int top = 0;  // behind it
+    for (int k = threadIdx.x & 63; k < n; k += 64) {
+      const uint32_t x = p[k];
+      if (x) top = max(top, 32 * (k % words) + 32 - __builtin_clz(x));
+    }
+    top = (int)__float_as_uint(wave_max(__uint_as_float((uint32_t)top)));
+    it.vis_end = clampi(it.nk - it.nq + min(top, it.nq), 0, it.nk);
+  }
   it.n_chunks = C > 1 ? max(1, (int)(((uint32_t)it.vis_end + it.chunk - 1) / (uint32_t)it.chunk)) : 1;
   // (all of it is the wave's, but the divisions leave it in vector registers)
   for (int* const p : {&it.kvh, &it.tile, &it.chunk, &it.c, &it.n_chunks, &it.slot, &it.record, &it.rows, &it.vis_end})
@@ -760,10 +793,12 @@ __device__ __forceinline__ void paged_few(const PagedArgs& a, char* const smem, 
   const int vis = row_limit(a, it, qi, kend);              // keys [0, vis) are seen
   const int vis0 = kTree ? clampi(it.nk - it.nq, 0, kend) : row_limit(a, it, q0, kend);  // by the first row (or every one)
   const int vis1 = min(it.vis_end, kend);                  // and by the last
-  const MaskRow mrow = mask_row<kTree>(a, it, qi);
+  MaskRow mrow = {nullptr, 0, 0};
   uint32_t word0 = 0;   // of the mask; as a rule the only one: 32 rows, so 32 new keys at most
   uint32_t some = ~0u;  // bit r: row r sees some key
   if constexpr (kTree) {
+    mrow = mask_row(a, it, qi);
+    asm volatile("" : "+v"(mrow.words), "+v"(mrow.first));
     word0 = mrow.row[0];
     some = (uint32_t)__builtin_amdgcn_ballot_w64(row_sees<true>(a, it, qi, 0.0f));
     asm volatile("" : "+v"(some));
@@ -1277,7 +1312,30 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
   // by the wave's first row (or every one)
   const int vis0 =
       kTree ? clampi(it.nk - it.nq, 0, kend) : row_limit(a, it, __builtin_amdgcn_readfirstlane(qi), kend);
-  const MaskRow mrow = mask_row<kTree>(a, it, qi);
+  // Masks of the blocks of 32 keys from the first that is not all seen on, for the tile's queries, lie in
+  // LDS behind the keys and values: a load from memory in the key loop would take its latency, for every
+  // block of new keys. `held`: the place of the lane's block 0, far below zero where they do
+  // not fit; then what such loads need is there instead. (Blocks that a wave sees whole take one
+  // read and one vote: two prompts with images, 1024 and 1001 new tokens, 28 heads, 106 us, with that 97.)
+  int held = 0, mine = 0;
+  if constexpr (kTree) {
+    constexpr int kSpare = (kSmem - 4 * kKBytes) / 4;
+    uint32_t* const spare = reinterpret_cast<uint32_t*>(smem + 4 * kKBytes);
+    const int b0 = max((vis0 - kbeg) >> 5, 0), per = 2 * ntiles - b0;
+    const int queries = small_div(h0 + it.rows - 1, inv_g) + 1;
+    mine = qi - q0;
+    if (queries * max(per, 0) <= kSpare) {
+      held = 4 * kKBytes + 4 * (mine * max(per, 0) - b0);
+      for (int k = tid; k < queries * per; k += 256) {
+        const int q = k / per, at = kbeg + 32 * (b0 + k - q * per);
+        spare[k] = mask_row(a, it, q0 + q).block(at, kend - at);
+      }
+    } else {
+      held = -(1 << 30);
+      if (tid == 0) *reinterpret_cast<MaskRow*>(spare) = mask_row(a, it, q0);
+    }
+    asm volatile("" : "+v"(held), "+v"(mine));
+  }
   int some = 1;  // does the lane's row see any key?
   if constexpr (kTree) {
     some = row_sees<true>(a, it, qi, 0.0f);
@@ -1301,8 +1359,13 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     const int kbase = kbeg + blk * kBK;
     if (kbase + kBK > vis0) {
       if constexpr (kTree) {
-        const int off = kbase - mrow.first, w = off >> 5;
-        const uint32_t bits = block_bits(mrow.word(w), mrow.word(w + 1), off, vis - kbase) >> (4 * lhalf);
+        uint32_t bits;
+        if (__builtin_amdgcn_readfirstlane(held) > -(1 << 29))
+          bits = *reinterpret_cast<const uint32_t*>(smem + held + 4 * blk);
+        else
+          bits = held_row(smem, mine).block(kbase, vis - kbase);
+        if (!__builtin_amdgcn_ballot_w64(bits != ~0u)) return;  // (in images most blocks are seen whole)
+        bits >>= 4 * lhalf;
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (!(bits >> (8 * (v >> 2) + (v & 3)) & 1)) sc[v] = -__builtin_inff();
@@ -1525,7 +1588,7 @@ __device__ __forceinline__ void paged_tile(const PagedArgs& a, char* const smem,
     for (int j = 8; j < 16; ++j) mfma_step<true>(oacc[j & 3], frag(j, 0, 1), pb[(j - 8) >> 2]);
     const int last_key = min(kend, kbeg + ntiles * kKT);
     if ((kTree || a.causal) && vis0 < last_key && any_nan(oacc)) {
-      paged_redo<kF8, false, kTree>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg, kBK, last_key, mrow);
+      paged_redo<kF8, false, kTree>(a, it.b, kvh, qf, oacc, m_run, l_run, c2, vis, kbeg, kBK, last_key, kTree ? mask_row(a, it, qi) : MaskRow{});
       if (lhalf) l_run = 0.0f;  // (the whole sum, once)
     }
   }

@@ -120,13 +120,36 @@ def test_any_bits(dtype, new, lens, g):
     assert (got[0] == 0).all()  # (the first sequence has no tokens before its new ones)
 
 
-def test_images_inside_a_prompt():
+# (128 rows of one query each hold more words than a tile keeps; 1500 cached keys are cut)
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("g,lens", [(3, [900, 150]), (1, [900, 150]), (1, [1800, 1650]), (7, [3000, 150])])
+def test_images_inside_a_prompt(dtype, g, lens):
     seen = []
     for n, ends in ((300, (40, 200, 230)), (150, (1, 150))):
         s = np.tril(np.ones((n, n), bool))
         s[ends[0]:ends[1], ends[0]:ends[1]] = True
         seen.append(s)
-    case([300, 150], [900, 150], 1, 3, 32, "bf16", seen, 10)
+    case([300, 150], lens, 1, g, 32, dtype, seen, 10)
+
+
+@pytest.mark.parametrize("B", [1, 70, 300])
+def test_batches_whose_chunks_are_rounded_up(B):
+    # lengths about one and a half shares: counts rounded up may be more than the places, and are not then
+    new = [40] * B if B < 300 else [9 + b % 3 for b in range(B)]
+    lens = [1100 + 7 * (b % 50) for b in range(B)] if B > 1 else [9000]
+    p = pu.Paged(lens, 2, 64, "bf16", k=[np.zeros((m, 2, du.DH), np.float32) for m in lens],
+                 v=[pu.bf16(np.full((m, 2, du.DH), 1.0) + np.arange(m)[:, None, None] % 3) for m in lens])
+    q = np.ones((sum(new), 14, du.DH), np.float32)
+    seen = trees(new)
+    got = du.attend(p, q, new, seen, 2)
+    # all scores are 0, so every output is the mean of the values seen: 1 + (0 + 1 + 2 of the keys) / their number
+    at = 0
+    for b, n in enumerate(new):
+        vis = du.visible(seen[b], n, lens[b])
+        want = (vis * (1 + np.arange(lens[b]) % 3)).sum(1) / vis.sum(1)
+        # weights of 1 are exact; the output's rounding is half a step, and so that of a float32 sum and quotient
+        assert np.abs(got[at:at + n] - want[:, None, None]).max() <= 2 * 2.0 ** -8 + 2.0 ** -10
+        at += n
 
 
 def test_masks_narrower_than_the_new_tokens():
