@@ -15,9 +15,9 @@
 //      worked on too: all at once they cost less than one after another. The last wave of
 //      a sequence to arrive makes the walk.
 // With probabilities, where a first child is rejected,
-//   3. verify_rest_kernel: chunk sums of what the rejection leaves of the row;
-//   4. verify_finish_kernel: the other children, of which each rejection is a pass over the row, and
-//      the token.
+//   3. verify_rest_kernel: chunk sums of what the rejection leaves of the row, and by the last
+//      workgroup of a sequence the other children, of which each rejection is a pass over the
+//      row, and the token.
 // What rejections leave is max(p - c q, 0) with a growing c (max(max(p - a q, 0) - b q, 0) =
 // max(p - (a + b) q, 0), as q >= 0), so nothing of a row is kept between them.
 #include <hip/hip_runtime.h>
@@ -92,7 +92,7 @@ struct VerifyArgs {
   float* top;   // [rows x chunks]
   double* sum;  // [rows x chunks], under the chunk's own maximum
   int32_t* out;      // [rows]: the token of a row; or its first child, accepted or rejected
-  uint32_t* arrived; // [B x kApart]: waves of a sequence that are done
+  uint32_t* arrived; // [B x kApart]: waves of a sequence that are done, and workgroups
   // with probabilities:
   float* most;     // [rows]: maximum and whole of a row
   double* whole;
@@ -375,6 +375,16 @@ __device__ __forceinline__ void load_values(const E* row, int c0, int vocab, flo
   unpack<kInOrder>(load_raw<kInOrder>(row, c0, vocab), c0, vocab, none, x);
 }
 
+__device__ __forceinline__ double how_many(const float (&x)[kPer], float m) {
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    n += x[k] == m;
+    asm volatile("" : "+v"(n));  // (one comparison at a time: sixteen results fill the scalar registers)
+  }
+  return n;
+}
+
 // Maximum and sums of two chunks of a row at a time, by waves that take
 // such pairs in turn, the next one's logits on their way.
 // Bound: instructions, some 16 a token and 5 a token of overhead: 521 rows of 131072 in bf16, 137 MB,
@@ -385,7 +395,7 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
   const int pairs = (a.chunks + 1) / 2;
   const uint32_t waves = gridDim.x * 4, all = (uint32_t)a.rows * (uint32_t)pairs;
   uint32_t i = blockIdx.x * 4 + (uint32_t)uniform((int)(threadIdx.x >> 6));
-  for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < (uint32_t)a.B; k += gridDim.x * 256) a.arrived[(int64_t)k * kApart] = 0;
+  for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < (uint32_t)a.B; k += gridDim.x * 256) a.arrived[(int64_t)k * kApart] = a.arrived[(int64_t)k * kApart + 1] = 0;
   int row, c;
   Raw<E> raw0, raw1;
   auto load = [&]() __attribute__((always_inline)) {
@@ -419,13 +429,16 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
     m = wave_max(m);
     double whole = 0.0;  // of the first chunk in the lower lanes, of the second in the upper
     if (m != neg_inf()) {
-      float under = m;
-      flatten(x1, under, h);
-      under = m;
-      flatten(x0, under, h);
-      const Fast f = fast_of(under, h);
-      const double w0 = sum_weights(x0, under, f, table);
-      whole = counted(wave_sums(w0, sum_weights(x1, under, f, table)));
+      double w0, w1;
+      if (h.greedy || m == __builtin_inff()) {  // only the largest count
+        w0 = how_many(x0, m);
+        w1 = how_many(x1, m);
+      } else {
+        const Fast f = fast_of(m, h);
+        w0 = sum_weights(x0, m, f, table);
+        w1 = sum_weights(x1, m, f, table);
+      }
+      whole = counted(wave_sums(w0, w1));
     }
     const int second = (threadIdx.x & 63) >> 5;
     if ((threadIdx.x & 31) == 0 && (second == 0 || two)) {
@@ -733,13 +746,13 @@ __global__ __launch_bounds__(64) void verify_rows_kernel(VerifyArgs args) {
   __shared__ double table[kSteps];
   __shared__ VerifyArgs held;  // (in LDS: twenty pointers leave no scalar registers)
   if (kProbs && threadIdx.x == 0) held = args;
-  load_table(table);
-  const VerifyArgs& a = kProbs ? held : args;
   // waves of the rows, then one of each sequence
   const int row = (int)blockIdx.x < args.rows ? (int)blockIdx.x : -1;
   Parts p;
-  load_parts(a, max(row, 0), 0, p);
-  const int b = row < 0 ? (int)blockIdx.x - args.rows : sequence_of(a, row);
+  load_parts(args, max(row, 0), 0, p);
+  const int b = row < 0 ? (int)blockIdx.x - args.rows : sequence_of(args, row);
+  load_table(table);  // (the loads before it come at the same time)
+  const VerifyArgs& a = kProbs ? held : args;
   if (b < 0) return;
   const int lo = uniform(clampi(a.offs[b], 0, a.rows)), n = uniform(clampi(a.offs[b + 1], lo, a.rows) - lo);
   const Heat h = heat_of(a, b);
@@ -783,46 +796,66 @@ __device__ __forceinline__ int row_at(const VerifyArgs& a, int b, int n) {
   return cur < n ? cur : -1;
 }
 
-template <typename E>
-__global__ __launch_bounds__(256) void verify_rest_kernel(VerifyArgs a) {
-  __shared__ double table[kSteps];
-  load_table(table);
-  const uint32_t at = blockIdx.x * 4 + (uint32_t)uniform((int)(threadIdx.x >> 6));
-  const int b = (int)(at / (uint32_t)a.chunks), c = (int)(at - (uint32_t)b * a.chunks);
-  if (b >= a.B) return;
-  const int lo = clampi(a.offs[b], 0, a.rows), n = clampi(a.offs[b + 1], lo, a.rows) - lo;
-  const int cur = row_at(a, b, n);
-  if (cur < 0) return;
-  const int row = lo + cur;
-  Heat h = heat_of(a, b);
-  h.greedy = false;
-  const double sum = rest_sum(row_of<E>(a, row), c * kChunk, a.vocab, uniform(a.most[row]), h, a.whole[row], table);
-  if ((threadIdx.x & 63) == 0) a.rest[at] = sum;
+// A chunk's sum, for and by workgroups on any XCD.
+__device__ __forceinline__ void put_rest(double* p, double x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ double get_rest(const double* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// Workgroup (b, g): chunks 4 g .. +3 of the row of sequence b where a first child is rejected; the
+// last of the sequence's goes on from there.
 template <typename E>
-__global__ __launch_bounds__(256) void verify_finish_kernel(VerifyArgs args) {
+__global__ __launch_bounds__(256) void verify_rest_kernel(VerifyArgs args) {
   __shared__ double table[kSteps];
   __shared__ VerifyArgs a;  // (as above)
+  __shared__ int last_s;
   if (threadIdx.x == 0) a = args;
   load_table(table);
-  const int b = blockIdx.x;
+  const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  const int groups = (args.chunks + 3) / 4;
+  const int b = (int)(blockIdx.x / (uint32_t)groups);
   const int lo = uniform(clampi(a.offs[b], 0, a.rows)), n = uniform(clampi(a.offs[b + 1], lo, a.rows) - lo);
   int cur = row_at(a, b, n);
   if (cur < 0) return;
   Heat h = heat_of(a, b);
   h.greedy = false;
-  const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   double* const rest = a.rest + (int64_t)b * a.chunks;
+  // the row cur, whose first child is rejected, and the child to ask next with its token (loaded before
+  // the sums, which take as long)
+  Row<E> r;
+  float m, u;
+  double cw;
+  int child, x;
+  auto enter = [&]() __attribute__((always_inline)) {
+    const int row = lo + cur;
+    r = row_of<E>(a, row);
+    m = uniform(a.most[row]);
+    cw = a.whole[row];
+    u = a.u_sample[row];
+    child = next_asked(a, lo, n, cur, clampi(uniform(a.out[row]) - kRejected, cur, n), x);
+  };
+  enter();
   int kept = uniform(a.n_kept[b]), token = -1;
+  {
+    const int c = ((int)blockIdx.x - b * groups) * 4 + wave;
+    if (c < a.chunks) {
+      const double sum = rest_sum(r, c * kChunk, a.vocab, m, h, cw, table);
+      if (lane == 0) put_rest(rest + c, sum);
+    }
+    asm volatile("" ::: "memory");
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (threadIdx.x == 0)
+      last_s = __hip_atomic_fetch_add(a.arrived + (int64_t)b * kApart + 1, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+               (uint32_t)groups - 1;
+    __syncthreads();
+    if (!uniform(last_s != 0)) return;
+  }
   bool have_rest = true;
   for (;;) {
-    // row cur, whose first child is rejected; the walk's rows up to it are kept
-    const int row = lo + cur;
-    const Row<E> r = row_of<E>(a, row);
-    const float m = uniform(a.most[row]);
-    double cw = a.whole[row], sw;
-    int child = clampi(uniform(a.out[row]) - kRejected, cur, n), x;
+    double sw;
     bool yes = false, last = false;
     for (;;) {
       if (!have_rest) {
@@ -833,27 +866,28 @@ __global__ __launch_bounds__(256) void verify_finish_kernel(VerifyArgs args) {
 #pragma unroll
           for (int i = 0; i < kPer; ++i) sum += w[i];
           sum = counted(of_lane(wave_scan(sum), 63));
-          if (lane == 0) rest[c] = sum;
+          if (lane == 0) put_rest(rest + c, sum);
         }
+        wait_vmcnt<0>();
         __syncthreads();
       }
       have_rest = false;
       sw = 0.0;
-      for (int c0 = 0; c0 < a.chunks; c0 += 64) sw += of_lane(wave_scan(c0 + lane < a.chunks ? rest[c0 + lane] : 0.0), 63);
-      child = last ? -1 : next_asked(a, lo, n, cur, child, x);
-      if (child >= 0) {
+      for (int c0 = 0; c0 < a.chunks; c0 += 64) sw += of_lane(wave_scan(c0 + lane < a.chunks ? get_rest(rest + c0 + lane) : 0.0), 63);
+      if (child >= 0 && !last) {
         yes = accepted<E>(a, r, lo + child, x, m, h, cw, sw, table);
         if (yes) break;
         cw += sw;
+        child = next_asked(a, lo, n, cur, child, x);
         continue;
       }
       // no child is left: a token of what is left of the row
       if (uniform(sw > 0.0)) {
-        const double target = (double)a.u_sample[row] * sw;
+        const double target = (double)u * sw;
         double base = 0.0, before = 0.0;
         int some = 0, chunk = -1;
         for (int c0 = 0; c0 < a.chunks && chunk < 0; c0 += 64) {
-          const double part[1] = {c0 + lane < a.chunks ? rest[c0 + lane] : 0.0};
+          const double part[1] = {c0 + lane < a.chunks ? get_rest(rest + c0 + lane) : 0.0};
           chunk = first_above(part, c0, target, base, before, some);
         }
         if (chunk < 0) {
@@ -876,7 +910,10 @@ __global__ __launch_bounds__(256) void verify_finish_kernel(VerifyArgs args) {
         f = uniform(a.out[lo + cur]);
       }
     }
-    if (f >= kRejected && f < kToken) continue;
+    if (f >= kRejected && f < kToken) {
+      enter();
+      continue;
+    }
     if (f >= kToken) token = f - kToken;  // a row without a child
     break;
   }
@@ -919,10 +956,7 @@ hipError_t launch(const VerifyArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((verify_rows_kernel<E, true>), waves, dim3(64), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(verify_rest_kernel<E>, blocks((int64_t)a.B * a.chunks), dim3(256), 0, stream, a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(verify_finish_kernel<E>, dim3(a.B), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(verify_rest_kernel<E>, dim3((unsigned)((int64_t)a.B * ((a.chunks + 3) / 4))), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
