@@ -42,7 +42,7 @@ def axes_of(pairs, n):
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("rows,heads,dim,pairs,axes", [
     (1, 1, 128, 64, 1), (5, 3, 128, 32, 3), (7, 4, 64, 32, 2), (3, 2, 80, 40, 3), (4, 5, 72, 36, 4), (9, 4, 96, 20, 1),
-    (2, 4, 256, 128, 2), (6, 4, 48, 5, 2), (3, 8, 254, 1, 1), (300, 9, 128, 64, 3), (3000, 30, 64, 16, 1), (2, 4, 2, 1, 1)])
+    (2, 4, 256, 128, 2), (6, 4, 48, 5, 2), (3, 8, 254, 1, 1), (300, 9, 128, 64, 3), (3000, 30, 64, 16, 1), (3000, 30, 128, 64, 3), (2, 4, 2, 1, 1)])
 def test_turn(dtype, interleaved, rows, heads, dim, pairs, axes):
     x = make(rows, heads, dim, dtype)
     rng = np.random.default_rng(1)

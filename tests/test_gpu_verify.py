@@ -132,6 +132,15 @@ def test_a_later_sibling_is_accepted_and_the_walk_goes_on():
     assert hit > 3
 
 
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("vocab", [262145, 1300001])
+def test_more_tokens_than_a_wave_holds_chunks_of(vocab, drawn):
+    # the row's whole is spread evenly, so its token lies in any chunk
+    c = Case([5, 4], vocab, torch.float32, drawn=drawn, seed=vocab, spread=0.5)
+    c.us[:] = np.linspace(0.05, 0.95, len(c.us))
+    c.check()
+
+
 @pytest.mark.parametrize("B,n", [(1, 1), (65, 2), (300, 3), (5000, 1)])
 def test_batches(B, n):
     new = [n if b % 7 else 0 for b in range(B)]
