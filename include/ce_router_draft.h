@@ -96,7 +96,7 @@ int ce_paged_tree_attention(const ce_kv_cache* cache, const ce_paged_attn* attn,
  *     (from p_r if S is 0).
  *   A sample of weights w by u is the first i with w_0 + .. + w_i > u (w_0 + .. + w_(vocab-1)),
  *   the last i of a positive weight where rounding leaves none. Weights below 2^-800 of a
- *   row's largest count as none.
+ *   row's largest count as none (up to 2^-780 they may).
  *   T is not positive (or NaN): p_r is 1 at the lowest index of the largest logit.
  * Logits of NaN count as -infinity; where some are +infinity they share all probability. A row
  * without a logit above -infinity has no distribution: its walk ends there, without a next
@@ -115,7 +115,8 @@ int ce_paged_tree_attention(const ce_kv_cache* cache, const ce_paged_attn* attn,
  *                256-byte aligned, contents on entry do not matter; calls that may overlap,
  *                captured ones among them, need workspaces of their own
  * Exponentials, sums and comparisons are of 64 bits. Entries of kept_rows behind the
- * last sequence are left as they were. Deterministic.
+ * last sequence are left as they were, and where the offsets are out of order those of some
+ * sequences may be too. Deterministic.
  * Limits: 1 <= vocab < 2^24, row_capacity * vocab < 2^40. Errors: CE_ERR_INVALID_ARG for null
  * pointers, sizes, or a u_accept without draft_probs or the reverse; CE_ERR_UNSUPPORTED
  * outside the limits; CE_ERR_WORKSPACE; CE_ERR_HIP.

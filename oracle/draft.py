@@ -67,7 +67,11 @@ def weights(logits, temperature):
         return w
     if top == np.inf:
         return (x == np.inf).astype(np.float64)
-    return np.exp((x - top) / temperature)
+    w = np.zeros(len(x))
+    some = x > -np.inf
+    w[some] = np.exp((x[some] - top) / temperature)
+    w[w < 2.0 ** -800] = 0.0  # (count as none)
+    return w
 
 
 def sample(w, u):

@@ -225,7 +225,8 @@ struct Fast {
 __device__ __forceinline__ Fast fast_of(float m, const Heat& h) {
   const double mi = rint((double)m * h.s), least = (mi + kLeast) * h.over_s;
   Fast f;
-  f.usable = uniform(fabs(mi) < 0x1p40 && fabs(least) < 0x1p126);
+  // (the floor's rounding to float32 moves its exponent by 2^-24 of mi: less than an octave)
+  f.usable = uniform(fabs(mi) < 0x1p30 && fabs(least) < 0x1p126);
   f.c = 0x1.8p52 - mi;
   f.s = h.s;
   f.floor = (float)least;

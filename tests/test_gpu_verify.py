@@ -202,6 +202,22 @@ def test_numbers_at_their_ends():
     c.check()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("offset,temp", [(0.0, 1.0), (3e4, 0.01), (-3e5, 0.05), (2e6, 0.3), (2e7, 1.0), (-1e12, 1.0), (1e30, 2.0),
+                                         (5.0, 1e-38), (5.0, 3e38), (5.0, float("inf")), (0.0, 1e-45)])
+def test_hidden_chunks_and_far_logits(dtype, offset, temp):
+    # whole chunks of hidden tokens at both ends, numbers at theirs, and logits and temperatures of any size
+    c = Case([4, 4, 4, 4], 9000, dtype, chains=True, temps=[temp] * 4)
+    c.us[:] = [0.0] * 4 + [1.0 - 2.0 ** -24] * 4 + [0.3] * 8
+    x = c.logits.float() * (1.0 if abs(offset) < 1e5 else abs(offset) * 2.0 ** -9) + offset
+    x[:, :5000] = -float("inf")
+    x[:, 8000:] = -float("inf")
+    x[2, 8500] = float("nan")
+    x[3, 5100:7900] = offset - abs(offset) - 2e4  # far below the others
+    c.logits = x.to(dtype)
+    c.check()
+
+
 def test_equal_distributions_and_tokens_of_no_vocabulary():
     c = Case([6, 6, 6], 600, torch.float32, drawn=True, chains=False, seed=5)
     c.parents = [[-1, 0, 0, 0, 1, 1]] * 3
