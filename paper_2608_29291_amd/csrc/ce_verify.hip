@@ -41,7 +41,6 @@ constexpr int kStepsLog2 = 7, kSteps = 1 << kStepsLog2;  // of an octave, in the
 constexpr double kLeast = -812.0 * kSteps;
 constexpr double kNone = 0x1p-800;
 
-
 constexpr int kApart = 32;  // words between counters, a cache line: arrivals at one line wait for each other
 
 __device__ const double kExpTable[kSteps] = {  // 2^(k / kSteps)
@@ -182,13 +181,18 @@ struct Heat {
   double s, over_s;  // and its inverse
   bool greedy;
 };
-__device__ __forceinline__ Heat heat_of(const VerifyArgs& a, int b) {
+__device__ __forceinline__ Heat heat_at(const VerifyArgs& a, int b) {  // (b: a lane's own)
   const float t = a.temps ? a.temps[b] : 1.0f;
   Heat h;
-  h.greedy = uniform(!(t > 0.0f));
+  h.greedy = !(t > 0.0f);
   const double heat = h.greedy ? 1.0 : (double)t;
   h.s = 0x1.71547652b82fep+7 / heat;  // kSteps log2 e
   h.over_s = 0x1.62e42fefa39efp-8 * heat;
+  return h;
+}
+__device__ __forceinline__ Heat heat_of(const VerifyArgs& a, int b) {
+  Heat h = heat_at(a, b);
+  h.greedy = uniform(h.greedy);
   return h;
 }
 
@@ -295,24 +299,44 @@ __device__ __forceinline__ void flatten(float (&x)[kPer], float& m, const Heat& 
   m = 0.0f;
 }
 
-// The sequence of a row, or -1. Every wave by itself.
-__device__ __forceinline__ int sequence_of(const VerifyArgs& a, int row) {
+// Of fewer than 64 sequences a lane holds one's first row and heat (lane B: the last one's end).
+struct Held {
+  int first;
+  Heat h;
+};
+__device__ __forceinline__ Held hold_sequences(const VerifyArgs& a) {
+  Held l = {};
+  if (a.B < 64) {
+    const int lane = threadIdx.x & 63;
+    l.first = a.offs[min(lane, a.B)];
+    l.h = heat_at(a, min(lane, a.B - 1));
+  }
+  return l;
+}
+
+// The sequence of a row and its heat; -1: none. Every wave by itself.
+__device__ __forceinline__ int sequence_of(const VerifyArgs& a, const Held& l, int row, Heat& h) {
   const int lane = threadIdx.x & 63;
-  if (a.B < 64) {  // the offset behind it is in a lane as well
-    const int o = a.offs[min(lane, a.B)];
-    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.B && o <= row));
+  if (a.B < 64) {
+    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.B && l.first <= row));
     if (n == 0) return -1;
-    return __builtin_amdgcn_readlane(o, n - 1) <= row && row < __builtin_amdgcn_readlane(o, n) ? n - 1 : -1;
+    const int b = n - 1;
+    h.s = of_lane(l.h.s, b);
+    h.over_s = of_lane(l.h.over_s, b);
+    h.greedy = __builtin_amdgcn_readlane(l.h.greedy, b) != 0;
+    return __builtin_amdgcn_readlane(l.first, b) <= row && row < __builtin_amdgcn_readlane(l.first, n) ? b : -1;
   }
   int lo = 0;
-  for (int step = a.B > 4096 ? 4096 : (a.B > 64 ? 64 : 1); step > 0; step >>= 6) {
+  for (int step = a.B > 4096 ? 4096 : 64; step > 0; step >>= 6) {
     const int i = lo + lane * step;
     const bool le = i < a.B && a.offs[i < a.B ? i : 0] <= row;
     const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(le));
     lo += (n > 0 ? n - 1 : 0) * step;
   }
   lo = uniform(lo);
-  return uniform(a.offs[lo] <= row && row < a.offs[lo + 1]) ? lo : -1;
+  if (!uniform(a.offs[lo] <= row && row < a.offs[lo + 1])) return -1;
+  h = heat_of(a, lo);
+  return lo;
 }
 
 template <typename E>
@@ -387,41 +411,44 @@ __device__ __forceinline__ double how_many(const float (&x)[kPer], float m) {
 }
 
 // Maximum and sums of two chunks of a row at a time, by waves that take
-// such pairs in turn, the next one's logits on their way.
-// Bound: instructions, some 16 a token and 5 a token of overhead: 521 rows of 131072 in bf16, 137 MB,
-// 47 us, where reading them alone takes 28; 272 of 100003 in float32, 109 MB, 27.
+// such pairs in turn, the next one's logits on their way. The sequences' rows and heats stay in the
+// lanes: looking them up for each pair anew cost a tenth of the time.
+// Bound: instructions, some 16 a token and 4 a token of overhead: 521 rows of 131072 in bf16, 137 MB, a
+// third of them with only the largest to count, 39 us, where reading them
+// alone takes 28; 272 of 100003 in float32, 109 MB, 25.
 template <typename E>
 __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
   __shared__ double table[kSteps];
   const int pairs = (a.chunks + 1) / 2;
   const uint32_t waves = gridDim.x * 4, all = (uint32_t)a.rows * (uint32_t)pairs;
   uint32_t i = blockIdx.x * 4 + (uint32_t)uniform((int)(threadIdx.x >> 6));
+  const int rows_on = (int)(waves / (uint32_t)pairs), pairs_on = (int)(waves - (uint32_t)rows_on * pairs);
+  int row = (int)(i / (uint32_t)pairs), pair = (int)(i - (uint32_t)row * pairs);
   for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < (uint32_t)a.B; k += gridDim.x * 256) a.arrived[(int64_t)k * kApart] = a.arrived[(int64_t)k * kApart + 1] = 0;
-  int row, c;
   Raw<E> raw0, raw1;
   auto load = [&]() __attribute__((always_inline)) {
-    row = (int)(i / (uint32_t)pairs);
-    c = (int)(i - (uint32_t)row * pairs) * 2;
+    const int c = 2 * pair;
     const E* const l = reinterpret_cast<const E*>(a.logits + (int64_t)row * a.ld);
     raw0 = load_raw<false>(l, c * kChunk, a.vocab);
     raw1 = load_raw<false>(l, (c + 1) * kChunk, a.vocab);  // (a chunk that is none: the last token)
   };
   if (i < all) load();
+  const Held held = hold_sequences(a);
   load_table(table);
-  int of = -1, b = -1;  // the row that b and h belong to
-  Heat h = {};
   while (i < all) {
-    if (row != of) {
-      of = row;
-      b = sequence_of(a, row);
-      if (b >= 0) h = heat_of(a, b);
-    }
+    Heat h = {};
+    const int b = sequence_of(a, held, row, h), c = 2 * pair;
     float x0[kPer], x1[kPer];
     unpack<false>(raw0, c * kChunk, a.vocab, neg_inf(), x0);
     unpack<false>(raw1, (c + 1) * kChunk, a.vocab, neg_inf(), x1);
     const int64_t to = (int64_t)row * a.chunks + c;
     const bool two = c + 1 < a.chunks;
     i += waves;
+    row += rows_on;
+    if ((pair += pairs_on) >= pairs) {
+      pair -= pairs;
+      ++row;
+    }
     if (i < all) load();
     if (b < 0) continue;
     float m = neg_inf();
@@ -751,12 +778,14 @@ __global__ __launch_bounds__(64) void verify_rows_kernel(VerifyArgs args) {
   const int row = (int)blockIdx.x < args.rows ? (int)blockIdx.x : -1;
   Parts p;
   load_parts(args, max(row, 0), 0, p);
-  const int b = row < 0 ? (int)blockIdx.x - args.rows : sequence_of(args, row);
+  const Held sequences = hold_sequences(args);
   load_table(table);  // (the loads before it come at the same time)
+  Heat h = {};
+  const int b = row < 0 ? (int)blockIdx.x - args.rows : sequence_of(args, sequences, row, h);
   const VerifyArgs& a = kProbs ? held : args;
   if (b < 0) return;
   const int lo = uniform(clampi(a.offs[b], 0, a.rows)), n = uniform(clampi(a.offs[b + 1], lo, a.rows) - lo);
-  const Heat h = heat_of(a, b);
+  if (row < 0) h = heat_of(a, b);
   const bool drawn = kProbs && !h.greedy;
   const int lane = threadIdx.x;
   if (row >= 0) {
