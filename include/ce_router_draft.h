@@ -101,8 +101,8 @@ int ce_paged_tree_attention(const ce_kv_cache* cache, const ce_paged_attn* attn,
  * Logits of NaN count as -infinity; where some are +infinity they share all probability. A row
  * without a logit above -infinity has no distribution: its walk ends there, without a next
  * token (-1). Drafted tokens outside [0, vocab) are not accepted, and not asked.
- *   logits       device dtype (CE_BF16 or CE_F32): row r at r * logits_ld elements, vocab of them;
- *                rows need no alignment beyond the element's
+ *   logits       device dtype (CE_BF16 or CE_F32): row_capacity rows, row r at r * logits_ld elements,
+ *                vocab of them; rows need no alignment beyond the element's
  *   temperature  device float32 [B] or NULL (1)
  *   draft_probs  device float32, row r at r * probs_ld, or NULL; negative and NaN count as 0
  *   u_accept     device float32 [row_capacity] in [0, 1); NULL without draft_probs

@@ -314,7 +314,12 @@ __device__ __forceinline__ Held hold_sequences(const VerifyArgs& a) {
   return l;
 }
 
-// The sequence of a row and its heat; -1: none. Every wave by itself.
+// Rows behind the last sequence's end are nobody's (a padded batch: their logits are not read).
+__device__ __forceinline__ int end_of(const VerifyArgs& a, const Held& l) {
+  return clampi(a.B < 64 ? __builtin_amdgcn_readlane(l.first, a.B) : uniform(a.offs[a.B]), 0, a.rows);
+}
+
+// The sequence of a row before the end and its heat; -1: none. Every wave by itself.
 __device__ __forceinline__ int sequence_of(const VerifyArgs& a, const Held& l, int row, Heat& h) {
   const int lane = threadIdx.x & 63;
   if (a.B < 64) {
@@ -421,7 +426,7 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
   __shared__ double table[kSteps];
   const int pairs = (a.chunks + 1) / 2;
   const uint32_t waves = gridDim.x * 4, all = (uint32_t)a.rows * (uint32_t)pairs;
-  uint32_t i = blockIdx.x * 4 + (uint32_t)uniform((int)(threadIdx.x >> 6));
+  const uint32_t i = blockIdx.x * 4 + (uint32_t)uniform((int)(threadIdx.x >> 6));
   const int rows_on = (int)(waves / (uint32_t)pairs), pairs_on = (int)(waves - (uint32_t)rows_on * pairs);
   int row = (int)(i / (uint32_t)pairs), pair = (int)(i - (uint32_t)row * pairs);
   for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < (uint32_t)a.B; k += gridDim.x * 256) a.arrived[(int64_t)k * kApart] = a.arrived[(int64_t)k * kApart + 1] = 0;
@@ -432,10 +437,11 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
     raw0 = load_raw<false>(l, c * kChunk, a.vocab);
     raw1 = load_raw<false>(l, (c + 1) * kChunk, a.vocab);  // (a chunk that is none: the last token)
   };
-  if (i < all) load();
+  if (i < all) load();  // (beside the offsets, that may put it behind the end)
   const Held held = hold_sequences(a);
+  const int end = end_of(a, held);
   load_table(table);
-  while (i < all) {
+  while (row < end) {
     Heat h = {};
     const int b = sequence_of(a, held, row, h), c = 2 * pair;
     float x0[kPer], x1[kPer];
@@ -443,13 +449,12 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
     unpack<false>(raw1, (c + 1) * kChunk, a.vocab, neg_inf(), x1);
     const int64_t to = (int64_t)row * a.chunks + c;
     const bool two = c + 1 < a.chunks;
-    i += waves;
     row += rows_on;
     if ((pair += pairs_on) >= pairs) {
       pair -= pairs;
       ++row;
     }
-    if (i < all) load();
+    if (row < end) load();
     if (b < 0) continue;
     float m = neg_inf();
 #pragma unroll
@@ -781,7 +786,7 @@ __global__ __launch_bounds__(64) void verify_rows_kernel(VerifyArgs args) {
   const Held sequences = hold_sequences(args);
   load_table(table);  // (the loads before it come at the same time)
   Heat h = {};
-  const int b = row < 0 ? (int)blockIdx.x - args.rows : sequence_of(args, sequences, row, h);
+  const int b = row < 0 ? (int)blockIdx.x - args.rows : row < end_of(args, sequences) ? sequence_of(args, sequences, row, h) : -1;
   const VerifyArgs& a = kProbs ? held : args;
   if (b < 0) return;
   const int lo = uniform(clampi(a.offs[b], 0, a.rows)), n = uniform(clampi(a.offs[b + 1], lo, a.rows) - lo);
@@ -841,11 +846,12 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(VerifyArgs args) {
   __shared__ double table[kSteps];
   __shared__ VerifyArgs a;  // (as above)
   __shared__ int last_s;
+  const int groups = (args.chunks + 3) / 4;
+  const int b = (int)(blockIdx.x / (uint32_t)groups);
+  if (uniform(args.at[b]) < 0) return;
   if (threadIdx.x == 0) a = args;
   load_table(table);
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const int groups = (args.chunks + 3) / 4;
-  const int b = (int)(blockIdx.x / (uint32_t)groups);
   const int lo = uniform(clampi(a.offs[b], 0, a.rows)), n = uniform(clampi(a.offs[b + 1], lo, a.rows) - lo);
   int cur = row_at(a, b, n);
   if (cur < 0) return;

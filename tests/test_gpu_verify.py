@@ -148,6 +148,14 @@ def test_batches(B, n):
     Case(new, 300, torch.bfloat16, seed=B).check()
 
 
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("B", [1, 3, 64, 100])
+def test_batches_that_are_mostly_padding(B, drawn):
+    # (more rows behind the last sequence than all of the chip's waves take at once)
+    c = Case([3, 0, 5, 1][:B] * (B // 4 + 1), 2100, torch.bfloat16, drawn=drawn, seed=B)
+    c.check(pad=7000)
+
+
 def test_chains_without_parents_and_no_temperature():
     c = Case([7, 1, 0, 20], 700, torch.bfloat16, chains=True)
     c.check(parents=False, temps=False)
