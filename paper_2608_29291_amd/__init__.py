@@ -1133,12 +1133,12 @@ def _spaced(x, name, dtype, heads, d):
     """Pointer of rows [n, heads, d] that may be spaced, and their stride in elements."""
     try:
         p = x.data_ptr()
-        if x.dtype is dtype and x.get_device() == _device() and not p & 15:
+        if x.is_cuda and x.dtype is dtype and x.get_device() == _device() and not p & 15:
             row = heads * d
             if x.is_contiguous() and not row & 7:
                 return p, row
             s = x.stride()
-            if x.is_cuda and s[2] == 1 and s[1] == d and s[0] >= row and not s[0] & 7:
+            if s[2] == 1 and s[1] == d and s[0] >= row and not s[0] & 7:
                 return p, s[0]
     except (AttributeError, TypeError):
         pass
