@@ -58,6 +58,7 @@ struct PagedArgs {
   unsigned long long token;     // of this call, 48 bits
   const uint32_t* mask;  // a tree's rows: who sees which new token, mask_words a row; else NULL
   int mask_words;
+  int short_keys;    // sequences of that many lengths from kPagedShort on go 32 rows to a tile, however many they have
   PagedPlan* plan;   // B > kPagedScan: the sequences, then the items, (whole) the chunk length and (slots) if half of the places are filled
 };
 
@@ -65,6 +66,8 @@ constexpr int kPagedScan = 256;    // sequences that a wave plans by itself (fou
 constexpr int kPagedFew = 32;     // (query, head) rows of a tile of single tokens
 constexpr int kPagedTile = 128;   // and of one of many rows
 constexpr int kPagedPlaces = 512; // places for workgroups: two on each CU
+constexpr int kPagedFewUnits = kPagedPlaces / 2; // tiles of 32 rows up to which a call's short sequences take such
+constexpr int kPagedShort = 96;    // least keys of these
 constexpr int kPagedRecord = 32;  // bytes of a cut unit's record
 constexpr int kPagedLevels = 3;    // sixteen chunks meet at a time, 512 at most
 
@@ -72,10 +75,11 @@ constexpr int kPagedLevels = 3;    // sixteen chunks meet at a time, 512 at most
 struct PagedGrid {
   int64_t items;
   int decode;
+  int few;        // a small call under a mask: its short sequences go 32 rows to a tile
   int cut_units;  // for the launch that adds chunks up, at most (0: no such launch)
   size_t plan_bytes, count_bytes, bytes;  // workspace: the plan, counters or records, partial results
 };
-PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys);
+PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys, bool tree);
 
 hipError_t launch_kv_reserve(ReserveArgs a, hipStream_t stream);
 hipError_t launch_kv_append(AppendArgs a, bool e4m3, hipStream_t stream);

@@ -57,7 +57,7 @@ int check_attn(const ce_kv_cache* c, const ce_paged_attn* at) {
 }
 
 PagedGrid grid_of(const ce_kv_cache* c, const ce_paged_attn* at) {
-  return paged_grid(c->B, at->n_heads, c->n_kv_heads, at->q_capacity, (int64_t)c->max_pages * c->page_size);
+  return paged_grid(c->B, at->n_heads, c->n_kv_heads, at->q_capacity, (int64_t)c->max_pages * c->page_size, false);
 }
 
 // mask: NULL, or a tree's

@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedArgs a) {
 
 }  // namespace
 
-PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
+PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys, bool tree) {
   PagedGrid p = {};
   if (q_cap <= 0) return p;
   // Single tokens: no more rows than sequences, and no more than eight rows of a
@@ -277,9 +277,10 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
   // over 2000 23.5 / 29.7, but 200 over 8000 62.6 / 47.4 (37.2 in a batch of one place).
   p.decode = q_cap <= B && H / Hkv <= 8;
   // every sequence with a query adds at most one tile that is not full
-  const int64_t rows = p.decode ? kPagedFew : kPagedTile;
-  const int64_t units = ((int64_t)q_cap * (H / Hkv) / rows + (B < q_cap ? B : q_cap)) * Hkv;
-  p.items = units;
+  auto tiles = [&](int rows) { return ((int64_t)q_cap * (H / Hkv) / rows + (B < q_cap ? B : q_cap)) * Hkv; };
+  const int64_t units = tiles(p.decode ? kPagedFew : kPagedTile);
+  p.few = tree && tiles(kPagedFew) <= kPagedFewUnits;
+  p.items = p.few ? tiles(kPagedFew) : units;
   if (B > kPagedScan) p.plan_bytes = ((size_t)(B + 1) * sizeof(PagedPlan) + 255) / 256 * 256;
   p.bytes = p.plan_bytes;
   if (max_keys >= 2 * kMinTile) {  // else nothing is cut
@@ -297,7 +298,7 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys) {
 
 hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
   if (a.q_cap <= 0) return hipSuccess;
-  const PagedGrid p = paged_grid(a.B, a.H, a.Hkv, a.q_cap, (int64_t)a.max_pages << a.page_log2);
+  const PagedGrid p = paged_grid(a.B, a.H, a.Hkv, a.q_cap, (int64_t)a.max_pages << a.page_log2, a.mask != nullptr);
   // Groups of 1, 4, 16, 32 neighbours: 512 queries over 8704 keys 75.5, 76.2, 79.2,
   // 79.9 us, four chunks of 2048 over 7000 to 10240 888, 883, 896, 881.
   const uint32_t group = 4;
@@ -305,6 +306,7 @@ hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
   const int64_t grid = (p.items + unit - 1) / unit * unit;
   a.grid = (uint32_t)grid;
   a.decode = p.decode;
+  a.short_keys = p.few ? kWholeFew - kPagedShort : 0;  // (such are never cut: the workspace is that of the other tiles)
   static std::atomic<uint64_t> calls{0};
   a.token = paged_token(calls.fetch_add(1, std::memory_order_relaxed) + 1);
   if (a.B > kPagedScan) {

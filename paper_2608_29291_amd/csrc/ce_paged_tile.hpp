@@ -45,7 +45,12 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 //
 // A call of single tokens (a.decode: no more rows than sequences) takes its rows 32 at
 // a time (paged_few); any other takes those of a sequence that has more than 32 in
-// tiles of 128 (paged_tile).
+// tiles of 128 (paged_tile). Under masks of bits a sequence of 96 to 639 keys, which is not
+// cut, goes 32 rows to a tile as well, four waves over its keys instead of one, where all such tiles
+// have a CU of their own: us, 28 / 4 heads, bf16, four trees of 64 over 64, 150, 300, 500 keys
+// 7.6, 10.2, 11.8, 16.4 / 8.3, 8.9, 10.1, 13.0; one of 26 7.0, 9.6, 11.3, 15.7 / 7.2, 8.4, 9.4, 11.8.
+// With 308 tiles 12.9 / 13.2 and, 8 bits, 14.1 / 15.6 (4 x 200 rows, 12 / 2 heads, 300 keys); from 700
+// keys on such tiles, cut, take 0.7 to 1.2 of the time.
 //
 // A unit is a row tile of a sequence for one key/value head; units are numbered
 // sequence by sequence, head by head, the last tiles first (under a causal mask they
@@ -87,7 +92,9 @@ struct Size {
   int qbase, nq, nk, tiles;
 };
 
-__device__ __forceinline__ bool is_few(const PagedArgs& a, int nq, int g) { return a.decode || nq * g <= kFew; }
+__device__ __forceinline__ bool is_few(const PagedArgs& a, int nq, int nk, int g) {
+  return a.decode || nq * g <= kFew || (uint32_t)(nk - kPagedShort) < (uint32_t)a.short_keys;
+}
 
 __device__ __forceinline__ int tile_rows(bool few) { return few ? kFew : kTileRows; }
 
@@ -96,7 +103,7 @@ __device__ __forceinline__ Size size_from(const PagedArgs& a, int q0, int q1, in
   s.qbase = clampi(q0, 0, a.q_cap);
   s.nq = clampi(q1, s.qbase, a.q_cap) - s.qbase;
   s.nk = clampi(len, 0, a.max_pages << a.page_log2);
-  const int few = is_few(a, s.nq, g);
+  const int few = is_few(a, s.nq, s.nk, g);
   s.tiles = (s.nq * g + tile_rows(few) - 1) >> (few ? kFewLog2 : kTileLog2);
   return s;
 }
@@ -127,7 +134,7 @@ __device__ __forceinline__ bool rounds_up(const PagedArgs& a, int L) { return a.
 // A sequence's chunks (a whole number of its waves' tiles).
 __device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, int L, bool half, bool near, int& C,
                                     int& chunk) {
-  const bool few = is_few(a, s.nq, g);
+  const bool few = is_few(a, s.nq, s.nk, g);
   if (few) {
     const int l = 2 * min(L, 1 << 29);  // (2^30: nothing is cut)
     C = s.nk < kWholeFew ? 1 : s.nk / max(half ? 2 * l : l, kMinFew);
@@ -157,7 +164,7 @@ __device__ __forceinline__ uint32_t whole_of(const PagedArgs& a, const Size& s, 
 
 // Its keys as the plan counts them, per unit.
 __device__ __forceinline__ float cost_of(const PagedArgs& a, const Size& s, int g) {
-  return (float)s.nk * (is_few(a, s.nq, g) ? 0.5f : 1.0f);
+  return (float)s.nk * (is_few(a, s.nq, s.nk, g) ? 0.5f : 1.0f);
 }
 
 // Its items, its partial results, the units that have such and their chunks.
@@ -344,9 +351,9 @@ __device__ __forceinline__ bool find_by_scan(const PagedArgs& a, int g, uint32_t
     }
     slots_to = wave_scan(sum_s);
     to = wave_scan(sum);
-    // more workgroups than the launch has, or slots than the workspace: where counts are
-    // rounded up too many of them were, else only where offsets are out of order. Then nothing is cut (every chunk of a cut unit
-    // must run) and what lies past the grid is left.
+    // More workgroups than the launch has, or slots than the workspace: too many counts were
+    // rounded up, so all are rounded down; or offsets are out of order, then nothing is cut (every
+    // chunk of a cut unit must run) and what lies past the grid is left.
     if (L == 1 << 30 ||
         (__builtin_amdgcn_readlane(to, 63) <= a.grid && __builtin_amdgcn_readlane(slots_to, 63) <= (uint32_t)kPagedPlaces))
       break;
@@ -439,7 +446,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, uint32_t at, Item&
   it.qbase = f.size.qbase;
   it.nq = f.size.nq;
   it.nk = f.size.nk;
-  it.few = is_few(a, it.nq, g);
+  it.few = is_few(a, it.nq, it.nk, g);
   int C = f.C;
   it.chunk = f.chunk;
   uint32_t u = at - f.before;

@@ -36,12 +36,12 @@ def device_mask(seen, words, rows, junk=0):
     return torch.from_numpy(m.view(np.int32)).cuda()
 
 
-def attend(p, q, new, seen, words, scale=DH ** -0.5, cache=None, ws=True, stream=None, junk=0, mask=None):
+def attend(p, q, new, seen, words, scale=DH ** -0.5, cache=None, ws=True, stream=None, junk=0, mask=None, pad=3):
     """ce_paged_tree_attention on bf16 rows q; rows behind the last one are checked to stay as they were."""
     import paper_2608_29291_amd as ce
     c = cache or p.cache()
     qd = torch.from_numpy(q).to(torch.bfloat16).cuda()
-    qd = torch.cat([qd, torch.zeros((3,) + qd.shape[1:], dtype=torch.bfloat16, device="cuda")])
+    qd = torch.cat([qd, torch.zeros((pad,) + qd.shape[1:], dtype=torch.bfloat16, device="cuda")])
     o = torch.full(qd.shape, 77.0, dtype=torch.bfloat16, device="cuda")
     off, lens = up(offsets(new)), torch.tensor(p.lens, dtype=torch.int32).cuda()
     mask = device_mask(seen, words, len(qd), junk) if mask is None else mask

@@ -93,6 +93,12 @@ def trees(new, seed=5):
 
 # few rows and many, a call of single tokens (no more rows than sequences with padding: 3 more
 # rows than needed, so B is large there), trees alone, over short and over cut caches
+# (many rows behind the last sequence: the call counts as a large one, and short sequences' rows
+# go 128 to a tile, not 32)
+PADS = [3, 12000]
+
+
+@pytest.mark.parametrize("pad", PADS)
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("new,lens,hkv,g,page,words", [
     ([1], [1], 1, 1, 16, 1),
@@ -104,32 +110,40 @@ def trees(new, seed=5):
     ([130, 70], [130, 400], 1, 4, 16, 5),
     ([2, 0, 1, 0, 0, 0, 0, 1], [900, 0, 33, 5, 0, 1, 2, 2100], 2, 4, 16, 1),
 ])
-def test_tree_attention(dtype, new, lens, hkv, g, page, words):
-    case(new, lens, hkv, g, page, dtype, trees(new), words)
+def test_tree_attention(dtype, new, lens, hkv, g, page, words, pad):
+    case(new, lens, hkv, g, page, dtype, trees(new), words, pad=pad)
 
 
+@pytest.mark.parametrize("pad", PADS)
+@pytest.mark.parametrize("words", [2, 5])
+def test_lengths_about_the_shortest_that_is_cut(words, pad):
+    case([40, 33, 64, 64, 20], [639, 640, 641, 600, 64], 2, 4, 16, "bf16", trees([40, 33, 64, 64, 20]), words, pad=pad)
+
+
+@pytest.mark.parametrize("pad", PADS)
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("new,lens,g", [([20, 45, 200], [20, 300, 517], 3), ([3, 7], [3, 2000], 2)])
-def test_any_bits(dtype, new, lens, g):
+def test_any_bits(dtype, new, lens, g, pad):
     # bits of any kind, behind the row itself too, and rows that see nothing at all
     rng = np.random.default_rng(11)
     seen = [rng.random((n, n)) < 0.3 for n in new]
     for s in seen:
         s[::4] = False
-    _, _, got = case(new, lens, 2, g, 16, dtype, seen, 7)
+    _, _, got = case(new, lens, 2, g, 16, dtype, seen, 7, pad=pad)
     assert (got[0] == 0).all()  # (the first sequence has no tokens before its new ones)
 
 
 # (128 rows of one query each hold more words than a tile keeps; 1500 cached keys are cut)
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("g,lens", [(3, [900, 150]), (1, [900, 150]), (1, [1800, 1650]), (7, [3000, 150])])
-def test_images_inside_a_prompt(dtype, g, lens):
+@pytest.mark.parametrize("pad", PADS)
+def test_images_inside_a_prompt(dtype, g, lens, pad):
     seen = []
     for n, ends in ((300, (40, 200, 230)), (150, (1, 150))):
         s = np.tril(np.ones((n, n), bool))
         s[ends[0]:ends[1], ends[0]:ends[1]] = True
         seen.append(s)
-    case([300, 150], lens, 1, g, 32, dtype, seen, 10)
+    case([300, 150], lens, 1, g, 32, dtype, seen, 10, pad=pad)
 
 
 @pytest.mark.parametrize("B", [1, 70, 300])
@@ -152,18 +166,19 @@ def test_batches_whose_chunks_are_rounded_up(B):
         at += n
 
 
-def test_masks_narrower_than_the_new_tokens():
+@pytest.mark.parametrize("pad", PADS)
+def test_masks_narrower_than_the_new_tokens(pad):
     seen = [np.ones((70, 70), bool)]
     p = pu.Paged([100], 1, 16, "bf16")
     q = pu.bf16(np.random.default_rng(0).standard_normal((70, 2, du.DH)))
-    got = du.attend(p, q, [70], seen, 2)
+    got = du.attend(p, q, [70], seen, 2, pad=pad)
     seen[0][:, 64:] = False  # token 64 on has no bit
     pu.check(got, *du.answer(p, q, [70], seen))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
-@pytest.mark.parametrize("n", [5, 60])
-def test_what_is_hidden_has_no_influence(dtype, n):
+@pytest.mark.parametrize("n,pad", [(5, 3), (60, 3), (60, 12000)])
+def test_what_is_hidden_has_no_influence(dtype, n, pad):
     """NaN, infinities and huge values in keys and values that no row, or not every row sees."""
     rng = np.random.default_rng(2)
     seen = od.masks(du.tree(rng, n))[0]
@@ -174,7 +189,7 @@ def test_what_is_hidden_has_no_influence(dtype, n):
     v[bad[1]] = np.nan if dtype == "e4m3" else np.inf
     p = pu.Paged([m], 1, 16, dtype, k=[k], v=[v])
     q = pu.bf16(rng.standard_normal((n, 4, du.DH)))
-    got = du.attend(p, q, [n], [seen], 2, junk=JUNK)
+    got = du.attend(p, q, [n], [seen], 2, junk=JUNK, pad=pad)
     want, top = du.answer(p, q, [n], [seen])
     with np.errstate(invalid="ignore"):
         inf = np.isinf(want)
@@ -183,15 +198,15 @@ def test_what_is_hidden_has_no_influence(dtype, n):
     assert np.isfinite(got[0]).all()
 
 
-@pytest.mark.parametrize("n", [3, 40])
-def test_a_row_that_sees_scores_of_minus_infinity_only(n):
+@pytest.mark.parametrize("n,pad", [(3, 3), (40, 3), (40, 12000)])
+def test_a_row_that_sees_scores_of_minus_infinity_only(n, pad):
     k = np.ones((n, 1, du.DH), np.float32)
     k[0] = -np.inf
     p = pu.Paged([n], 1, 16, "bf16", k=[k])
     q = np.ones((n, 2, du.DH), np.float32)
     seen = np.eye(n, dtype=bool)
     seen[1] = False
-    got = du.attend(p, q, [n], [seen], 2)
+    got = du.attend(p, q, [n], [seen], 2, pad=pad)
     assert np.isnan(got[0]).all() and (got[1] == 0).all() and np.isfinite(got[2:]).all()
 
 
