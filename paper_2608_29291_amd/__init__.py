@@ -219,6 +219,7 @@ _DTYPE_CODE = {torch.bfloat16: CE_BF16, torch.float32: CE_F32}
 _TORCH_DTYPE = {CE_BF16: torch.bfloat16, CE_F32: torch.float32}
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 _device = torch._C._cuda_getDevice  # torch.cuda.current_device() once CUDA is initialised
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _dtype_code(t) -> int:
@@ -284,9 +285,9 @@ def _why_not(t, name, dtype, numel, shape, rows_min) -> str:
     return f"{name}: {t.shape[0]} rows, need at least {rows_min}"
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device=None) -> Optional[int]:
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(_device())
+        return _raw_stream(_device() if device is None else device)
     return stream.cuda_stream
 
 
@@ -951,12 +952,13 @@ def _scratch(need, device, stream):
 
 def _mask(mask, device, rows):
     """Pointer and words a row of a mask [>= rows, words] of 4-byte integers."""
-    if mask.dim() != 2 or mask.dtype not in (torch.int32, torch.uint32):
+    dtype = mask.dtype
+    if mask.dim() != 2 or (dtype is not _I32 and dtype is not torch.uint32):
         raise ValueError("mask must be a matrix [rows, words] of 4-byte integers")
-    words = mask.shape[1]
-    if mask.shape[0] < rows:
-        raise ValueError(f"mask has {mask.shape[0]} rows, q {rows}")
-    return _vec(mask, "mask", device, rows * words, mask.dtype), words
+    n, words = mask.shape
+    if n < rows:
+        raise ValueError(f"mask has {n} rows, q {rows}")
+    return _vec(mask, "mask", device, rows * words, dtype), words
 
 
 def ce_paged_attention(cache: KVCache, q, o, q_offsets, lens, causal, scale, ws=None, stream=None):
@@ -982,32 +984,40 @@ class Drafts:
     rows: Optional[int] = None
 
     def c(self) -> CEDrafts:
-        if self.offsets is None or self.offsets.dim() != 1:
+        """The arguments, checked, with the device that they are on."""
+        offsets, parents, tokens, rows = self.offsets, self.parents, self.tokens, self.rows
+        if offsets is None or offsets.dim() != 1:
             raise ValueError("offsets must be a vector [B+1]")
-        op = _chk(self.offsets, "offsets", _I32, 2)
+        if not offsets.is_cuda:
+            _chk(offsets, "offsets")  # (no device is asked for)
         dev = _device()
-        sized = self.parents if self.parents is not None else self.tokens
-        if self.rows is None and sized is None:
-            raise ValueError("rows must be given where neither parents nor tokens is")
-        rows = sized.numel() if self.rows is None else int(self.rows)
-        return CEDrafts(self.offsets.numel() - 1, rows, op,
-                        None if self.parents is None else _vec(self.parents, "parents", dev, rows),
-                        None if self.tokens is None else _vec(self.tokens, "tokens", dev, rows))
+        op = _vec(offsets, "offsets", dev, 2)
+        if rows is None:
+            sized = tokens if parents is None else parents
+            if sized is None:
+                raise ValueError("rows must be given where neither parents nor tokens is")
+            rows = sized.numel()
+        else:
+            rows = int(rows)
+        c = CEDrafts(offsets.numel() - 1, rows, op, None if parents is None else _vec(parents, "parents", dev, rows),
+                     None if tokens is None else _vec(tokens, "tokens", dev, rows))
+        c.device = dev
+        return c
 
 
 def ce_draft_masks(drafts: Drafts, mask=None, positions=None, base=None, status=None, stream=None):
     """Bits of every row and its ancestors into mask [rows, words] (int32 or uint32, 1 to 64
     words), base[b] + the number of ancestors into positions int32 [rows]; status: 4-byte
     integer tensor for the CE_DEV_* bits."""
-    dc, dev = drafts.c(), _device()
-    rows = dc.row_capacity
+    dc = drafts.c()
+    dev, rows = dc.device, dc.row_capacity
     mp, words = (None, 1) if mask is None else _mask(mask, dev, rows)
     if status is not None and status.dtype not in (torch.int32, torch.uint32):
         raise ValueError("status must be a 4-byte integer tensor")
     _check(lib.ce_draft_masks(ctypes.byref(dc), words, None if base is None else _vec(base, "base", dev, dc.B), mp,
                               None if positions is None else _vec(positions, "positions", dev, rows),
                               None if status is None else _vec(status, "status", dev, 1, status.dtype),
-                              _stream(stream)), "ce_draft_masks")
+                              _stream(stream, dev)), "ce_draft_masks")
 
 
 def ce_paged_tree_attention(cache: KVCache, q, o, q_offsets, lens, mask, scale, ws=None, stream=None):
@@ -1051,8 +1061,8 @@ def ce_verify_drafts(drafts: Drafts, logits, u_sample, kept_rows, n_kept, next_t
     chosen, with them (float32 [rows, vocab], and u_accept) the children of a row were
     drawn from its row; u_sample, u_accept float32 [rows] in [0, 1). Without a workspace
     (alloc_verify_workspace) scratch comes from torch's allocator."""
-    dc, dev = drafts.c(), _device()
-    rows, B = dc.row_capacity, dc.B
+    dc = drafts.c()
+    dev, rows, B = dc.device, dc.row_capacity, dc.B
     lp, vocab, ld = _matrix(logits, "logits", dev, (torch.bfloat16, _F32), rows)
     pp, pld = None, 0
     if draft_probs is not None:
@@ -1068,7 +1078,7 @@ def ce_verify_drafts(drafts: Drafts, logits, u_sample, kept_rows, n_kept, next_t
         None if temperature is None else _vec(temperature, "temperature", dev, B, _F32), pp, pld,
         None if u_accept is None else _vec(u_accept, "u_accept", dev, rows, _F32), _vec(u_sample, "u_sample", dev, rows, _F32),
         _vec(kept_rows, "kept_rows", dev, rows), _vec(n_kept, "n_kept", dev, B), _vec(next_token, "next_token", dev, B),
-        None if ws is None else _chk(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
+        None if ws is None else _chk(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream, dev)),
         "ce_verify_drafts")
 
 
@@ -1079,7 +1089,7 @@ def ce_kv_keep(cache: KVCache, offsets, start, kept_rows, n_kept, stream=None):
     dev, B = cc.device, cc.B
     rows = kept_rows.numel()
     _check(lib.ce_kv_keep(ctypes.byref(cc), _vec(offsets, "offsets", dev, B + 1), rows, _vec(start, "start", dev, B),
-                          _vec(kept_rows, "kept_rows", dev, rows), _vec(n_kept, "n_kept", dev, B), _stream(stream)),
+                          _vec(kept_rows, "kept_rows", dev, rows), _vec(n_kept, "n_kept", dev, B), _stream(stream, dev)),
            "ce_kv_keep")
 
 
@@ -1096,7 +1106,7 @@ def ce_kv_trim(cache: KVCache, lens, start, n_kept, free_pages, free_count, lens
         ctypes.byref(cc), lp, _vec(start, "start", dev, B), _vec(n_kept, "n_kept", dev, B),
         _vec(free_pages, "free_pages", dev, cc.n_pages), cp, lp if lens_out is None else _vec(lens_out, "lens_out", dev, B),
         cp if free_count_out is None else _vec(free_count_out, "free_count_out", dev, 1),
-        None if status is None else _vec(status, "status", dev, 1, status.dtype), _stream(stream)), "ce_kv_trim")
+        None if status is None else _vec(status, "status", dev, 1, status.dtype), _stream(stream, dev)), "ce_kv_trim")
 
 
 # ----------------------------------------------------------------------------
@@ -1166,7 +1176,7 @@ def ce_rotary(rotary: Rotary, x, y, positions, index=None, inverse=False, stream
     desc = CERotaryDesc(rows, heads, d, rotary.n_pairs, axes, rotary.layout, 1 if inverse else 0, code, n, rotary.freq_ptr,
                         rotary.axis_ptr, _vec(positions, "positions", dev, axes * n),
                         None if index is None else _vec(index, "index", dev, rows))
-    _check(lib.ce_rotary(ctypes.byref(desc), xp, xl, yp, yl, _stream(stream)), "ce_rotary")
+    _check(lib.ce_rotary(ctypes.byref(desc), xp, xl, yp, yl, _stream(stream, dev)), "ce_rotary")
 
 
 __all__ = [
