@@ -429,7 +429,10 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
   const uint32_t i = blockIdx.x * 4 + (uint32_t)uniform((int)(threadIdx.x >> 6));
   const int rows_on = (int)(waves / (uint32_t)pairs), pairs_on = (int)(waves - (uint32_t)rows_on * pairs);
   int row = (int)(i / (uint32_t)pairs), pair = (int)(i - (uint32_t)row * pairs);
-  for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < (uint32_t)a.B; k += gridDim.x * 256) a.arrived[(int64_t)k * kApart] = a.arrived[(int64_t)k * kApart + 1] = 0;
+  for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < (uint32_t)a.B; k += gridDim.x * 256) {
+    a.arrived[(int64_t)k * kApart] = a.arrived[(int64_t)k * kApart + 1] = 0;
+    if (a.probs) a.at[k] = -1;  // (offsets out of order leave sequences without a walk)
+  }
   Raw<E> raw0, raw1;
   auto load = [&]() __attribute__((always_inline)) {
     const int c = 2 * pair;
@@ -825,7 +828,7 @@ __global__ __launch_bounds__(64) void verify_rows_kernel(VerifyArgs args) {
   walk<kProbs>(a, b, lo, n, drawn);
 }
 
-// A row of a sequence's walk with a rejection, -1 if there is none (or the offsets are out of order).
+// A row of a sequence's walk with a rejection, -1 if there is none.
 __device__ __forceinline__ int row_at(const VerifyArgs& a, int b, int n) {
   const int cur = uniform(a.at[b]);
   return cur < n ? cur : -1;
@@ -873,7 +876,7 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(VerifyArgs args) {
     child = next_asked(a, lo, n, cur, clampi(uniform(a.out[row]) - kRejected, cur, n), x);
   };
   enter();
-  int kept = uniform(a.n_kept[b]), token = -1;
+  int kept = uniform(clampi(a.n_kept[b], 0, n)), token = -1;
   {
     const int c = ((int)blockIdx.x - b * groups) * 4 + wave;
     if (c < a.chunks) {

@@ -51,7 +51,7 @@ class Case:
             nxt.append(t)
         return kept, n_kept, nxt
 
-    def run(self, parents=True, temps=True, ws=True, stream=None, logits=None, probs=None, pad=3, rest=True):
+    def run(self, parents=True, temps=True, ws=True, stream=None, logits=None, probs=None, pad=3, rest=True, fill=0xff):
         n = len(self.tokens)
         flat = [p for t in self.parents for p in t]
         i32 = lambda x: du.up(np.concatenate([np.array(x, np.int32), np.zeros(pad, np.int32)]))
@@ -67,7 +67,7 @@ class Case:
         w = None
         if ws:
             w = ce.alloc_verify_workspace(d, logits.shape[1], probs is not None)
-            w.fill_(0xff)  # what is on entry must not matter
+            w.fill_(fill)  # what is on entry must not matter
         torch.cuda.synchronize()
         ce.ce_verify_drafts(d, logits, f32(self.us), kept, nk, nxt, temperature=du.up(self.temps) if temps else None,
                             draft_probs=probs, u_accept=f32(self.ua) if probs is not None else None, ws=w, stream=stream)
@@ -264,12 +264,35 @@ def test_repeats_streams_and_scratch():
         c.check(ws=False, stream=torch.cuda.Stream())
 
 
+@pytest.mark.parametrize("drawn", [False, True])
+def test_one_workspace_for_calls_of_many_kinds(drawn):
+    # what a call leaves in its workspace is any content to the next
+    cases = [Case(new, vocab, torch.bfloat16, drawn=drawn, seed=i)
+             for i, (new, vocab) in enumerate([([9, 3], 7000), ([5] * 70, 500), ([1], 30000), ([9, 0, 3], 7000)])]
+    ws = torch.full((1 << 22,), 0x5a, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        for c in cases:
+            want, n = c.answer(), len(c.tokens)
+            i32 = lambda x: du.up(np.array(x, np.int32))
+            kept, nk, nxt = i32([55] * n), i32([-9] * len(c.new)), i32([-9] * len(c.new))
+            ce.ce_verify_drafts(ce.Drafts(du.up(c.off), i32([p for t in c.parents for p in t]), i32(c.tokens)), c.logits.cuda(),
+                                du.up(c.us), kept, nk, nxt, draft_probs=du.up(c.probs) if drawn else None,
+                                u_accept=du.up(c.ua) if drawn else None, ws=ws)
+            np.testing.assert_array_equal(kept.cpu().numpy(), want[0])
+            assert nk.tolist() == want[1] and nxt.tolist() == want[2]
+
+
 def test_offsets_out_of_order_stay_in_bounds():
     c = Case([10, 10, 10], 500, torch.float32, drawn=True)
     want = c.answer()
     for off in ([0, 25, 5, 30], [-3, 10, 20, 1 << 30], [7, 7, 7, 7], [30, 20, 10, 0]):
         c.off = np.array(off, np.int32)
-        c.run(rest=False)
+        for pad in (3, 5000):
+            for fill in (0xff, 0):
+                kept, n_kept, _ = c.run(rest=False, pad=pad, fill=fill)
+                # (a sequence whose rows are not its own has no walk: its outputs stay as they were)
+                assert all(k == -9 or 0 <= k <= len(c.tokens) + pad for k in n_kept), n_kept
+                assert ((kept == 55) | (kept == -1) | ((kept >= 0) & (kept < len(c.tokens) + pad))).all()
     c.off = du.offsets(c.new)
     got = c.run()
     np.testing.assert_array_equal(got[0], want[0])
