@@ -117,7 +117,7 @@ int ce_paged_tree_attention(const ce_kv_cache* cache, const ce_paged_attn* attn,
  * Exponentials, sums and comparisons are of 64 bits. Entries of kept_rows behind the
  * last sequence are left as they were, and where the offsets are out of order those of some
  * sequences may be too. Deterministic.
- * Limits: 1 <= vocab < 2^24, row_capacity * vocab < 2^40. Errors: CE_ERR_INVALID_ARG for null
+ * Limits: 1 <= vocab < 2^24, row_capacity * vocab < 2^40, B * ceil(vocab / 4096) < 2^24. Errors: CE_ERR_INVALID_ARG for null
  * pointers, sizes, or a u_accept without draft_probs or the reverse; CE_ERR_UNSUPPORTED
  * outside the limits; CE_ERR_WORKSPACE; CE_ERR_HIP.
  */

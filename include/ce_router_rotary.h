@@ -31,7 +31,8 @@ enum { CE_ROTARY_HALVES = 0, CE_ROTARY_PAIRS = 1 };
  *             kept_idx); NULL: token r. A row whose token is outside [0, n_positions)
  *             is not turned
  * Limits: head_dim even, at most 256, 1 <= n_pairs <= head_dim / 2, 1 <= n_axes <= 4,
- * n_heads < 2^16.
+ * n_heads < 2^16, rows * n_heads < 2^31, and fewer than 2^32 threads (rows * ceil(n_heads / 4) below
+ * 2^24 - 1 needs no more at any width; pairs by eights allow 2^29).
  */
 typedef struct ce_rotary_desc {
   int32_t rows;

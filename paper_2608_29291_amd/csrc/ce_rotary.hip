@@ -267,6 +267,9 @@ extern "C" int ce_rotary(const ce_rotary_desc* d, const void* x, int64_t x_ld, v
   a.turning = d->n_pairs / n;
   a.lanes = a.turning + (x == y ? 0 : rest / n);
   const bool many = (int64_t)d->rows * d->n_heads * a.lanes * n * elem >= (int64_t)1 << 23;  // 32 MB, read and written
+  // (a launch has fewer than 2^32 threads)
+  if ((int64_t)d->rows * (many ? (d->n_heads + 3) / 4 : d->n_heads) / (256 / a.lanes) >= ((int64_t)1 << 24) - 1)
+    return CE_ERR_UNSUPPORTED;
   const bool pairs = d->layout == CE_ROTARY_PAIRS;
   const hipError_t e = d->dtype == CE_BF16 ? launch_by_width<uint16_t>(a, n, pairs, many, static_cast<hipStream_t>(stream))
                                            : launch_by_width<float>(a, n, pairs, many, static_cast<hipStream_t>(stream));

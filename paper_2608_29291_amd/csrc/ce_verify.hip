@@ -1006,7 +1006,7 @@ int check_sizes(const ce_drafts* d, int32_t vocab) {
   if (s != CE_OK) return s;
   if (vocab < 1) return CE_ERR_INVALID_ARG;
   if (vocab >= 1 << 24 || (int64_t)d->row_capacity * vocab >= (int64_t)1 << 40 ||
-      (int64_t)d->B * chunks_of(vocab) >= (int64_t)1 << 30)
+      (int64_t)d->B * ((chunks_of(vocab) + 3) / 4) >= (int64_t)1 << 24)  // (workgroups of 256 in one launch)
     return CE_ERR_UNSUPPORTED;
   return CE_OK;
 }

@@ -107,6 +107,8 @@ def test_verify_refusals():
     for kw in ({"vocab": 1 << 24, "ld": 1 << 24, "pld": 1 << 24}, {"dtype": ce.CE_E4M3}, {"ld": 1 << 32}, {"pld": 1 << 32}):
         assert verify(d, **kw) == UNS, kw
     assert verify(drafts(row_capacity=(1 << 24) - 1), vocab=1 << 17, ld=1 << 17, pld=1 << 17) == UNS
+    big = dict(vocab=1100000, ld=1100000, pld=1100000)  # (more workgroups than a launch may have)
+    assert verify(drafts(B=65535), **big) == UNS and size(drafts(B=65535), vocab=1100000) == 0
     need = size(d)
     assert 0 < size(d, probs=0) < need
     assert verify(d, ws=None) == verify(d, ws=FAKE + 16) == verify(d, ws_bytes=need - 1) == WS
@@ -147,6 +149,7 @@ def test_rotary_refusals():
     for kw in ({"head_dim": 258}, {"head_dim": 129}, {"n_pairs": 65}, {"n_axes": 5}, {"dtype": ce.CE_E4M3}, {"n_heads": 1 << 16},
                {"rows": 1 << 30}):
         assert rotary(**kw) == UNS, kw
+    assert rotary(rows=1 << 25, n_heads=1, head_dim=256, n_pairs=1, freqs=[1.0], y=2 * FAKE) == UNS
     assert rotary(rows=0, x=None, y=None) == 0
 
 
