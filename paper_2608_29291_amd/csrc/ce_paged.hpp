@@ -66,8 +66,12 @@ constexpr int kPagedScan = 256;    // sequences that a wave plans by itself (fou
 constexpr int kPagedFew = 32;     // (query, head) rows of a tile of single tokens
 constexpr int kPagedTile = 128;   // and of one of many rows
 constexpr int kPagedPlaces = 512; // places for workgroups: two on each CU
-constexpr int kPagedFewUnits = kPagedPlaces / 2; // tiles of 32 rows up to which a call's short sequences take such
-constexpr int kPagedShort = 96;    // least keys of these
+// Tiles of 32 rows up to which a call's short sequences take such: those that are not cut, and
+// those of up to kPagedLong keys; the least keys of both.
+constexpr int kPagedFewUnits = kPagedPlaces / 2;
+constexpr int kPagedFewest = 96;
+constexpr int kPagedLong = 8192;
+constexpr int kPagedShort = 96;
 constexpr int kPagedRecord = 32;  // bytes of a cut unit's record
 constexpr int kPagedLevels = 3;    // sixteen chunks meet at a time, 512 at most
 
@@ -75,7 +79,7 @@ constexpr int kPagedLevels = 3;    // sixteen chunks meet at a time, 512 at most
 struct PagedGrid {
   int64_t items;
   int decode;
-  int few;        // a small call under a mask: its short sequences go 32 rows to a tile
+  int short_keys;  // keys below which a sequence goes 32 rows to a tile (a small call under a mask), or 0
   int cut_units;  // for the launch that adds chunks up, at most (0: no such launch)
   size_t plan_bytes, count_bytes, bytes;  // workspace: the plan, counters or records, partial results
 };

@@ -279,8 +279,9 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys, bool tr
   // every sequence with a query adds at most one tile that is not full
   auto tiles = [&](int rows) { return ((int64_t)q_cap * (H / Hkv) / rows + (B < q_cap ? B : q_cap)) * Hkv; };
   const int64_t units = tiles(p.decode ? kPagedFew : kPagedTile);
-  p.few = tree && tiles(kPagedFew) <= kPagedFewUnits;
-  p.items = p.few ? tiles(kPagedFew) : units;
+  const int64_t few = tiles(kPagedFew);
+  p.short_keys = !tree || few > kPagedFewUnits ? 0 : (few > kPagedFewest ? kWholeFew : kPagedLong);
+  p.items = p.short_keys ? few : units;
   if (B > kPagedScan) p.plan_bytes = ((size_t)(B + 1) * sizeof(PagedPlan) + 255) / 256 * 256;
   p.bytes = p.plan_bytes;
   if (max_keys >= 2 * kMinTile) {  // else nothing is cut
@@ -288,7 +289,8 @@ PagedGrid paged_grid(int B, int H, int Hkv, int q_cap, int64_t max_keys, bool tr
     if (p.decode) {
       p.count_bytes = (size_t)kPagedLevels * kPagedPlaces * sizeof(unsigned long long);
     } else {  // a cut unit has two chunks at least
-      p.cut_units = (int)(units < kPagedPlaces / 2 ? units : kPagedPlaces / 2);
+      const int64_t cut = p.short_keys > kWholeFew ? few : units;  // (shorter ones are not cut)
+      p.cut_units = (int)(cut < kPagedPlaces / 2 ? cut : kPagedPlaces / 2);
       p.count_bytes = ((size_t)(kPagedPlaces / 2 + 1) * kPagedRecord + 255) / 256 * 256;
     }
     p.bytes += p.count_bytes + (size_t)kPagedPlaces * (p.decode ? kSlotBytes<true> : kSlotBytes<false>);
@@ -306,7 +308,7 @@ hipError_t launch_paged_attention(PagedArgs a, bool e4m3, hipStream_t stream) {
   const int64_t grid = (p.items + unit - 1) / unit * unit;
   a.grid = (uint32_t)grid;
   a.decode = p.decode;
-  a.short_keys = p.few ? kWholeFew - kPagedShort : 0;  // (such are never cut: the workspace is that of the other tiles)
+  a.short_keys = p.short_keys ? p.short_keys - kPagedShort : 0;
   static std::atomic<uint64_t> calls{0};
   a.token = paged_token(calls.fetch_add(1, std::memory_order_relaxed) + 1);
   if (a.B > kPagedScan) {

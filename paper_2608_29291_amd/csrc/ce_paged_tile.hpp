@@ -45,12 +45,16 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 //
 // A call of single tokens (a.decode: no more rows than sequences) takes its rows 32 at
 // a time (paged_few); any other takes those of a sequence that has more than 32 in
-// tiles of 128 (paged_tile). Under masks of bits a sequence of 96 to 639 keys, which is not
-// cut, goes 32 rows to a tile as well, four waves over its keys instead of one, where all such tiles
-// have a CU of their own: us, 28 / 4 heads, bf16, four trees of 64 over 64, 150, 300, 500 keys
-// 7.6, 10.2, 11.8, 16.4 / 8.3, 8.9, 10.1, 13.0; one of 26 7.0, 9.6, 11.3, 15.7 / 7.2, 8.4, 9.4, 11.8.
-// With 308 tiles 12.9 / 13.2 and, 8 bits, 14.1 / 15.6 (4 x 200 rows, 12 / 2 heads, 300 keys); from 700
-// keys on such tiles, cut, take 0.7 to 1.2 of the time.
+// tiles of 128 (paged_tile). Under masks of bits short sequences of small calls go 32 rows to a tile as
+// well, four waves over their keys instead of one:
+//   * of 96 to 639 keys, which are not cut, where all such tiles have a CU of their own: us, 28 / 4 heads,
+//     bf16, four trees of 64 over 64, 150, 300, 500 keys 7.6, 10.2, 11.8, 16.4 / 8.3, 8.9, 10.1, 13.0; one of
+//     26 7.0, 9.6, 11.3, 15.7 / 7.2, 8.4, 9.4, 11.8. With 308 tiles 12.9 / 13.2 and, 8 bits, 14.1 / 15.6 (4 x 200
+//     rows, 12 / 2 heads, 300 keys);
+//   * of up to 8191, in calls of at most 96 such tiles: 12 / 2 heads, bf16, a tree of 26 over 1100, 2500, 4000,
+//     8000, 16000 keys 13.1, 15.0, 14.8, 17.7, 23.6 / 12.0, 12.4, 12.6, 14.3, 22.3; 42 such calls of up to 96 tiles
+//     over 700 to 8000 keys on average 0.88 to 1.00 of the time, 1.11 at most; of 100 to 256 tiles 0.97 to 1.14, of
+//     16000 keys 0.9 to 1.5.
 //
 // A unit is a row tile of a sequence for one key/value head; units are numbered
 // sequence by sequence, head by head, the last tiles first (under a causal mask they

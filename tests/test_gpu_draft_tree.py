@@ -114,6 +114,13 @@ def test_tree_attention(dtype, new, lens, hkv, g, page, words, pad):
     case(new, lens, hkv, g, page, dtype, trees(new), words, pad=pad)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new,lens,hkv,g,words", [([26, 9], [8191, 8192], 1, 6, 1), ([40, 3, 200], [2500, 8193, 700], 1, 4, 7),
+                                                  ([5, 12, 70, 1], [4000, 640, 1100, 7000], 2, 6, 3)])
+def test_small_calls_over_long_caches(dtype, new, lens, hkv, g, words):
+    case(new, lens, hkv, g, 64, dtype, trees(new), words)
+
+
 @pytest.mark.parametrize("pad", PADS)
 @pytest.mark.parametrize("words", [2, 5])
 def test_lengths_about_the_shortest_that_is_cut(words, pad):
