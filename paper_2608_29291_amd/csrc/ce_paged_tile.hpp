@@ -47,7 +47,7 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? l
 // a time (paged_few); any other takes those of a sequence that has more than 32 in
 // tiles of 128 (paged_tile). Under masks of bits short sequences of small calls go 32 rows to a tile as
 // well, four waves over their keys instead of one:
-//   * of 96 to 639 keys, which are not cut, where all such tiles have a CU of their own: us, 28 / 4 heads,
+//   * of 96 to 639 keys, as a rule not cut, where all such tiles have a CU of their own: us, 28 / 4 heads,
 //     bf16, four trees of 64 over 64, 150, 300, 500 keys 7.6, 10.2, 11.8, 16.4 / 8.3, 8.9, 10.1, 13.0; one of
 //     26 7.0, 9.6, 11.3, 15.7 / 7.2, 8.4, 9.4, 11.8. With 308 tiles 12.9 / 13.2 and, 8 bits, 14.1 / 15.6 (4 x 200
 //     rows, 12 / 2 heads, 300 keys);
@@ -141,7 +141,10 @@ __device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, in
   const bool few = is_few(a, s.nq, s.nk, g);
   if (few) {
     const int l = 2 * min(L, 1 << 29);  // (2^30: nothing is cut)
-    C = s.nk < kWholeFew ? 1 : s.nk / max(half ? 2 * l : l, kMinFew);
+    // (where a second launch adds the chunks of short sequences up: 12.5 us whole, 11.8 cut, at 560 and 630 keys; 420
+    // and 500 keys +1.5%, 260 and 330 +10%)
+    const int whole = a.short_keys > kWholeFew ? 2 * kMinTile : kWholeFew;
+    C = s.nk < whole ? 1 : s.nk / max(half ? 2 * l : l, kMinFew);
     if (C > kMeet && (s.nk <= kMeet * kMaxMeet || C <= kMostOver)) C = kMeet;
   } else {
     const int l = max(L, kMinTile);

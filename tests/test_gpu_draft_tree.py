@@ -116,7 +116,8 @@ def test_tree_attention(dtype, new, lens, hkv, g, page, words, pad):
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("new,lens,hkv,g,words", [([26, 9], [8191, 8192], 1, 6, 1), ([40, 3, 200], [2500, 8193, 700], 1, 4, 7),
-                                                  ([5, 12, 70, 1], [4000, 640, 1100, 7000], 2, 6, 3)])
+                                                  ([5, 12, 70, 1], [4000, 640, 1100, 7000], 2, 6, 3),
+                                                  ([26, 40, 9], [511, 512, 600], 1, 6, 2)])
 def test_small_calls_over_long_caches(dtype, new, lens, hkv, g, words):
     case(new, lens, hkv, g, 64, dtype, trees(new), words)
 
