@@ -115,8 +115,9 @@ int ce_paged_tree_attention(const ce_kv_cache* cache, const ce_paged_attn* attn,
  *                256-byte aligned, contents on entry do not matter; calls that may overlap,
  *                captured ones among them, need workspaces of their own
  * Exponentials, sums and comparisons are of 64 bits. Entries of kept_rows behind the
- * last sequence are left as they were, and where the offsets are out of order those of some
- * sequences may be too. Deterministic.
+ * last sequence are left as they were. Where the offsets are out of order a sequence of which some
+ * rows are another's has no walk: n_kept 0, next_token -1, and its entries of kept_rows
+ * may be left as they were. Deterministic.
  * Limits: 1 <= vocab < 2^24, row_capacity * vocab < 2^40, B * ceil(vocab / 4096) < 2^24. Errors: CE_ERR_INVALID_ARG for null
  * pointers, sizes, or a u_accept without draft_probs or the reverse; CE_ERR_UNSUPPORTED
  * outside the limits; CE_ERR_WORKSPACE; CE_ERR_HIP.

@@ -466,7 +466,10 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(VerifyArgs a) {
   int row = (int)(i / (uint32_t)pairs), pair = (int)(i - (uint32_t)row * pairs);
   for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < (uint32_t)a.B; k += gridDim.x * 256) {
     a.arrived[(int64_t)k * kApart] = a.arrived[(int64_t)k * kApart + 1] = 0;
-    if (a.probs) a.at[k] = -1;  // (offsets out of order leave sequences without a walk)
+    // (offsets out of order leave sequences without a walk)
+    a.n_kept[k] = 0;
+    a.next[k] = -1;
+    if (a.probs) a.at[k] = -1;
   }
   Raw<E> raw0, raw1;
   auto load = [&]() __attribute__((always_inline)) {
