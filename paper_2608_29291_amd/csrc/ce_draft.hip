@@ -29,6 +29,70 @@ using namespace scan;
 __device__ __forceinline__ int parent_of(int p, int i) { return p < 0 || p >= i ? -1 : p; }
 
 constexpr int kStaged = 8192;  // rows whose words and exits LDS holds
+constexpr int kLater = 2048;   // and of the rows behind them, at a time
+
+// The word of row j, of which `up` is the parent, and the parent that it leaves its 32 rows by. Every lane
+// of the 32 must call it.
+__device__ __forceinline__ void link(int up, int j, uint32_t& m, int& exit) {
+  const int first = j & ~31;
+  int p = up >= first ? up & 31 : j & 31;  // (a row without one here points at itself)
+  m = 1u << (j & 31);
+#pragma unroll
+  for (int r = 0; r < 5; ++r) {
+    m |= (uint32_t)__shfl((int)m, p, 32);
+    p = __shfl(p, p, 32);
+  }
+  exit = __shfl(up >= first ? -1 : up, p, 32);
+}
+
+// Masks and positions of the rows behind the first kStaged of a sequence, by one workgroup, in order. No mask
+// has bits of these rows (they are 64 words at most), so a row's mask is that of the row by which its walk
+// leaves its kLater rows, and its position follows that row's: 64 steps a row at most, however far the
+// first ancestor is. One workgroup's latency bounds it: positions of a chain of 65536 rows 0.9 ms, with masks
+// of 64 words 4.2; of 2^20 rows 10.4 ms (parent by parent to the root that is 2^39 steps).
+__device__ __forceinline__ void later_rows(const DraftMaskArgs& a, int lo, int n, int base, uint32_t* lds) {
+  static_assert(kStaged >= 64 * 32 && kStaged % 32 == 0 && kLater % 256 == 0, "");
+  uint32_t* const own = lds;
+  int* const out = reinterpret_cast<int*>(lds + kLater);
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int t0 = kStaged; t0 < n; t0 += kLater) {
+    const int here = min(kLater, n - t0);
+    for (int k0 = 0; k0 < here; k0 += 256) {
+      const int j = t0 + k0 + tid;
+      uint32_t m;
+      int exit;
+      link(j < n ? (a.parents ? parent_of(a.parents[lo + j], j) : j - 1) : -1, j, m, exit);
+      own[k0 + tid] = m;
+      out[k0 + tid] = exit;
+    }
+    __syncthreads();
+    for (int k0 = 0; k0 < here; k0 += 256) {
+      const int k = k0 + tid, i = t0 + k;
+      int depth = 0, exit = -1;  // rows from i to the exit
+      if (i < n) {
+        depth = __builtin_popcount(own[k]);
+        exit = out[k];
+        while (exit >= t0) {
+          const int at = exit - t0;
+          depth += __builtin_popcount(own[at]);
+          exit = out[at];
+        }
+        if (a.positions) a.positions[lo + i] = (int)((exit < 0 ? (uint32_t)base - 1 : (uint32_t)a.positions[lo + exit]) + (uint32_t)depth);
+      }
+      if (a.mask) {
+        const int w0 = i & ~63, all = min(64, n - w0) * a.words;  // (none behind the last row)
+        uint32_t* const to = a.mask + (int64_t)(lo + w0) * a.words;
+        const uint32_t* const from = a.mask + (int64_t)lo * a.words;
+        for (int c0 = 0; c0 < all; c0 += 64) {
+          const int c = c0 + lane, r = min(c / a.words, 63);
+          const int e = __shfl(exit, r);
+          if (c < all) to[c] = e < 0 ? 0 : from[(int64_t)e * a.words + (c - r * a.words)];
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
 
 __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
   // words of the rows and their exits, `staged` of each
@@ -37,16 +101,16 @@ __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
   int16_t* const out = reinterpret_cast<int16_t*>(lds + a.staged);
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int lo = clampi(a.offs[b], 0, a.rows);
-  const int n = clampi(a.offs[b + 1], lo, a.rows) - lo;
+  const int all = clampi(a.offs[b + 1], lo, a.rows) - lo;
   const int base = a.base ? a.base[b] : 0;
-  const bool staged = n <= a.staged;
+  const int n = min(all, a.staged);  // (of a longer sequence the rows that LDS holds, by one workgroup)
+  const int turns = all > n ? 1 : gridDim.y;
   int done = 0;  // rows that are staged
   // rows 256 y .., and on from there by as many as the workgroups of the sequence take
-  for (int i0 = blockIdx.y * 256; i0 < n; i0 += gridDim.y * 256) {
+  for (int i0 = blockIdx.y * 256; i0 < n && (int)blockIdx.y < turns; i0 += turns * 256) {
     const int i = i0 + tid;
     uint32_t m = 0;
     int exit = -1;
-    if (!staged) done = i0;  // (a longer sequence than LDS holds: only the words of these rows)
     for (int j0 = done; j0 <= i0; j0 += 4 * 256) {
       int up[4];
 #pragma unroll
@@ -57,20 +121,10 @@ __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if (j0 + 256 * k > i0) break;
-        // the word of row j, and the parent that it leaves its 32 rows by
-        const int j = j0 + 256 * k + tid, first = j & ~31;
-        int p = up[k] >= first ? up[k] & 31 : j & 31;  // (a row without one here points at itself)
-        m = 1u << (j & 31);
-#pragma unroll
-        for (int r = 0; r < 5; ++r) {
-          m |= (uint32_t)__shfl((int)m, p, 32);
-          p = __shfl(p, p, 32);
-        }
-        exit = __shfl(up[k] >= first ? -1 : up[k], p, 32);
-        if (staged) {
-          own[j] = m;
-          out[j] = (int16_t)exit;
-        }
+        const int j = j0 + 256 * k + tid;
+        link(up[k], j, m, exit);
+        own[j] = m;
+        out[j] = (int16_t)exit;
       }
     }
     done = i0 + 256;
@@ -91,20 +145,14 @@ __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
         if (a.mask && w < a.words) row[w] = m;
         if (exit < 0) break;
         w = exit >> 5;
-        if (staged) {
-          m = own[exit];
-          exit = out[exit];
-        } else {  // parent by parent
-          m = 0;
-          int j = exit;
-          for (; j >= 0 && j >> 5 == w; j = a.parents ? parent_of(a.parents[lo + j], j) : j - 1) m |= 1u << (j & 31);
-          exit = j;
-        }
+        m = own[exit];
+        exit = out[exit];
       }
       if (a.positions) a.positions[lo + i] = (int)((uint32_t)base + (uint32_t)depth);
     }
     __syncthreads();
   }
+  if (all > n && blockIdx.y == 0) later_rows(a, lo, all, base, lds);
 }
 
 // CE_DEV_* bits of the trees. One workgroup.
