@@ -60,9 +60,9 @@ typedef struct ce_drafts {
  *               ce_rotary takes them
  *   status      device uint32 [1] out, or NULL: CE_DEV_* bits of this call
  * Rows behind the last sequence are left as they were. Deterministic, but where the offsets
- * are out of order (a row that lies in two sequences may have bits of both). The rows behind the
- * first 8192 of a sequence take their turn 2048 at a time: a chain of 65536 rows 0.9 ms, and
- * with masks of 64 words 4.2.
+ * are out of order (a row that lies in two sequences may have bits of both). A sequence of
+ * more than 8192 rows is worked on 2048 at a time: positions of a chain of 65536 0.6 ms, with
+ * masks of 64 words 4.2.
  * Errors: CE_ERR_INVALID_ARG for null pointers / sizes, CE_ERR_UNSUPPORTED outside the
  * limits, CE_ERR_HIP.
  */

@@ -29,7 +29,7 @@ using namespace scan;
 __device__ __forceinline__ int parent_of(int p, int i) { return p < 0 || p >= i ? -1 : p; }
 
 constexpr int kStaged = 8192;  // rows whose words and exits LDS holds
-constexpr int kLater = 2048;   // and of the rows behind them, at a time
+constexpr int kTurn = 2048;    // of a longer sequence, at a time
 
 // The word of row j, of which `up` is the parent, and the parent that it leaves its 32 rows by. Every lane
 // of the 32 must call it.
@@ -45,18 +45,18 @@ __device__ __forceinline__ void link(int up, int j, uint32_t& m, int& exit) {
   exit = __shfl(up >= first ? -1 : up, p, 32);
 }
 
-// Masks and positions of the rows behind the first kStaged of a sequence, by one workgroup, in order. No mask
-// has bits of these rows (they are 64 words at most), so a row's mask is that of the row by which its walk
-// leaves its kLater rows, and its position follows that row's: 64 steps a row at most, however far the
-// first ancestor is. One workgroup's latency bounds it: positions of a chain of 65536 rows 0.9 ms, with masks
-// of 64 words 4.2; of 2^20 rows 10.4 ms (parent by parent to the root that is 2^39 steps).
-__device__ __forceinline__ void later_rows(const DraftMaskArgs& a, int lo, int n, int base, uint32_t* lds) {
-  static_assert(kStaged >= 64 * 32 && kStaged % 32 == 0 && kLater % 256 == 0, "");
+// Masks and positions of a sequence longer than LDS holds, by one workgroup, kTurn rows at a time. Masks have bits of
+// the first kTurn rows only (64 words at most), so a later row's mask is that of the row by which its walk leaves
+// its kTurn, and its position follows that row's: 64 steps a row at most, however far the first ancestor is.
+// One workgroup's latency bounds it: positions of a chain of 65536 rows 0.6 ms, with masks of 64 words 4.2; of
+// 2^20 rows 9.5 ms (parent by parent to the root that is 2^39 steps).
+__device__ __forceinline__ void long_sequence(const DraftMaskArgs& a, int lo, int n, int base, uint32_t* lds) {
+  static_assert(kTurn >= 64 * 32 && kTurn % 256 == 0 && 4 * kTurn <= 3 * kStaged, "");
   uint32_t* const own = lds;
-  int* const out = reinterpret_cast<int*>(lds + kLater);
+  int* const out = reinterpret_cast<int*>(lds + kTurn);
   const int tid = threadIdx.x, lane = tid & 63;
-  for (int t0 = kStaged; t0 < n; t0 += kLater) {
-    const int here = min(kLater, n - t0);
+  for (int t0 = 0; t0 < n; t0 += kTurn) {
+    const int here = min(kTurn, n - t0);
     for (int k0 = 0; k0 < here; k0 += 256) {
       const int j = t0 + k0 + tid;
       uint32_t m;
@@ -70,13 +70,7 @@ __device__ __forceinline__ void later_rows(const DraftMaskArgs& a, int lo, int n
       const int k = k0 + tid, i = t0 + k;
       int depth = 0, exit = -1;  // rows from i to the exit
       if (i < n) {
-        depth = __builtin_popcount(own[k]);
-        exit = out[k];
-        while (exit >= t0) {
-          const int at = exit - t0;
-          depth += __builtin_popcount(own[at]);
-          exit = out[at];
-        }
+        for (exit = i; exit >= t0; exit = out[exit - t0]) depth += __builtin_popcount(own[exit - t0]);
         if (a.positions) a.positions[lo + i] = (int)((exit < 0 ? (uint32_t)base - 1 : (uint32_t)a.positions[lo + exit]) + (uint32_t)depth);
       }
       if (a.mask) {
@@ -87,6 +81,13 @@ __device__ __forceinline__ void later_rows(const DraftMaskArgs& a, int lo, int n
           const int c = c0 + lane, r = min(c / a.words, 63);
           const int e = __shfl(exit, r);
           if (c < all) to[c] = e < 0 ? 0 : from[(int64_t)e * a.words + (c - r * a.words)];
+        }
+        if (t0 == 0) {  // and their words over these zeros
+          asm volatile("" ::: "memory");
+          wait_vmcnt<0>();
+          if (i < n)
+            for (int e = i; e >= 0; e = out[e])
+              if (e >> 5 < a.words) a.mask[(int64_t)(lo + i) * a.words + (e >> 5)] = own[e];
         }
       }
     }
@@ -101,13 +102,15 @@ __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
   int16_t* const out = reinterpret_cast<int16_t*>(lds + a.staged);
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int lo = clampi(a.offs[b], 0, a.rows);
-  const int all = clampi(a.offs[b + 1], lo, a.rows) - lo;
+  const int n = clampi(a.offs[b + 1], lo, a.rows) - lo;
   const int base = a.base ? a.base[b] : 0;
-  const int n = min(all, a.staged);  // (of a longer sequence the rows that LDS holds, by one workgroup)
-  const int turns = all > n ? 1 : gridDim.y;
+  if (n > a.staged) {
+    if (blockIdx.y == 0) long_sequence(a, lo, n, base, lds);
+    return;
+  }
   int done = 0;  // rows that are staged
   // rows 256 y .., and on from there by as many as the workgroups of the sequence take
-  for (int i0 = blockIdx.y * 256; i0 < n && (int)blockIdx.y < turns; i0 += turns * 256) {
+  for (int i0 = blockIdx.y * 256; i0 < n; i0 += gridDim.y * 256) {
     const int i = i0 + tid;
     uint32_t m = 0;
     int exit = -1;
@@ -152,7 +155,6 @@ __global__ __launch_bounds__(256) void draft_masks_kernel(DraftMaskArgs a) {
     }
     __syncthreads();
   }
-  if (all > n && blockIdx.y == 0) later_rows(a, lo, all, base, lds);
 }
 
 // CE_DEV_* bits of the trees. One workgroup.
