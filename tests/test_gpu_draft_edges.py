@@ -4,6 +4,8 @@ import pytest
 import torch
 
 import draft_util as du
+import paged_util as pu
+from oracle import draft as od
 from test_gpu_verify import Case
 
 pytestmark = pytest.mark.gpu
@@ -97,3 +99,29 @@ def test_a_chain_of_a_million_rows_takes_no_walk_to_its_root(parents):
     np.testing.assert_array_equal(pos, np.concatenate([np.arange(n) + 3, [9, 10, 10, 11] if parents else [9, 10, 11, 12]]))
     assert (mask[64:n] == 0xffffffff).all()
     np.testing.assert_array_equal(mask[:64], plain_masks(list(range(-1, 63)), 2)[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("B,hkv,g", [(300, 2, 4), (257, 1, 7), (600, 1, 2)])
+@pytest.mark.parametrize("several", [False, True])
+def test_single_rows_of_more_sequences_than_a_wave_plans(dtype, B, hkv, g, several):
+    # no more rows than sequences: the kernel of single tokens behind the launch that plans
+    rng = np.random.default_rng(B + several)
+    new = np.ones(B, int)
+    if several:  # some with two to four, as many of none
+        order = rng.permutation(B)
+        new[order[:20]], new[order[20:40]], new[order[40:100]] = 2, 4, 0
+        new[order[100:120]] = 0
+    assert new.sum() <= B
+    lens = [int(n + x) for n, x in zip(new, np.exp(rng.uniform(0, np.log(3000), B)).astype(int) - 1)]
+    for b, m in ((0, 511), (1, 512), (2, 639), (3, 640), (4, 0), (5, 1)):
+        lens[b] = m
+    seen = [od.masks(du.tree(rng, n))[0] if n else np.zeros((0, 0), bool) for n in new]
+    for s in seen[::3]:
+        s[:1] = False
+    p = pu.Paged(lens, hkv, 32, dtype, seed=B)
+    q = pu.bf16(rng.standard_normal((new.sum(), hkv * g, du.DH)))
+    got = du.attend(p, q, new, seen, 1, junk=0xdeadbeef, pad=0)
+    pu.check(got, *du.answer(p, q, new, seen))
+    blind = [b for b in range(B) if len(seen[b]) and lens[b] <= new[b] and not seen[b][0].any()]
+    assert blind and all((got[new[:b].sum()] == 0).all() for b in blind)
