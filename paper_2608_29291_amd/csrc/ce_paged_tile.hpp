@@ -141,8 +141,9 @@ __device__ __forceinline__ void cut(const PagedArgs& a, const Size& s, int g, in
   const bool few = is_few(a, s.nq, s.nk, g);
   if (few) {
     const int l = 2 * min(L, 1 << 29);  // (2^30: nothing is cut)
-    // (where a second launch adds the chunks of short sequences up: 12.5 us whole, 11.8 cut, at 560 and 630 keys; 420
-    // and 500 keys +1.5%, 260 and 330 +10%)
+    // (in calls of at most kPagedFewest tiles: where a second launch adds the chunks up 12.5 us whole, 11.8 cut, at 560
+    // and 630 keys; 420 and 500 keys +1.5%, 260 and 330 +10%. Single tokens, whose chunks meet in the launch: 1 to 16
+    // sequences, three layouts of heads, 540 to 639 keys, bf16 9.4 to 10.0 / 8.6 to 9.2, 8 bits 10.3 to 11.0 / 9.2 to 10.5)
     const int whole = a.short_keys > kWholeFew ? 2 * kMinTile : kWholeFew;
     C = s.nk < whole ? 1 : s.nk / max(half ? 2 * l : l, kMinFew);
     if (C > kMeet && (s.nk <= kMeet * kMaxMeet || C <= kMostOver)) C = kMeet;
